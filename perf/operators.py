@@ -204,7 +204,7 @@ def prepare(case, seed):
     elif case["op"] == "labels":
         if calls:
             f = lambda *shape: torch.empty(*shape, device="cuda")
-            s["a"], s["e"], s["lse"] = f(n), f(n), f(n)
+            s["a"], s["e"], s["stats"] = f(n), f(n), f(n, 2)
             s["tv"] = f(n, case["top"]) if case["top"] else None
             s["ti"] = torch.empty(n, case["top"], dtype=torch.int32, device="cuda") if case["top"] else None
             s["ws"] = torch.empty(isp.label_logprob_workspace(n, case["classes"], case["top"]), dtype=torch.uint8, device="cuda")
@@ -253,11 +253,11 @@ def _own_labels(s, case):
         outs, grads = ((a, e), (s["da"], s["de"])) if s["de"] is not None else ((a,), (s["da"],))
         return (a.detach(), e.detach(), *top, torch.autograd.grad(outs, s["z"], grads)[0])
     isp = s["isp"]
-    isp.label_logprob(s["z"], s["labels"], s["a"], s["e"], lse=s["lse"], top_logprob=s["tv"], top_index=s["ti"], workspace=s["ws"])
+    isp.label_logprob(s["z"], s["labels"], s["a"], s["e"], stats=s["stats"], top_logprob=s["tv"], top_index=s["ti"], workspace=s["ws"])
     out = (s["a"], s["e"]) if s["tv"] is None else (s["a"], s["e"], s["tv"], s["ti"])
     if not case["train"]:
         return out
-    isp.label_logprob_backward(s["z"], s["labels"], s["lse"], s["da"], s["dz"], entropy=s["e"], d_entropy=s["de"])
+    isp.label_logprob_backward(s["z"], s["labels"], s["stats"], s["da"], s["dz"], entropy=s["e"], d_entropy=s["de"])
     return (*out, s["dz"])
 
 
