@@ -82,6 +82,11 @@ typedef enum {
 #define ISP_OP_DOT 1     /* f(z) = z */
 #define ISP_OP_ONE 2     /* f(z) = 1: plain aggregation through the fused path */
 
+/* element types of the operators that take more than fp32 (layer norm, label log probabilities, attention) */
+#define ISP_F32 0
+#define ISP_BF16 1
+#define ISP_F16 2
+
 /* Summary of a handle's row classes and work partition (all counts are rows unless named). */
 typedef struct {
   int64_t n_rows, n_cols, nnz;
@@ -300,6 +305,68 @@ isp_status isp_spmm_reduce(const isp_csr_t* A, const float* X, int64_t ldx, int3
  */
 isp_status isp_spmm_reduce_backward(isp_csr_t* A, const float* dY, int64_t lddy, int32_t d, int reduce,
                                     const int32_t* arg, float* dX, int64_t lddx, void* stream);
+
+/*
+ * Layer norm over the rows of a dense matrix: with the row's mean and rstd = (mean of (x - mean)^2 + eps)^-1/2,
+ *   Y[i, c] = (X[i, c] - mean_i) rstd_i weight[c] + bias[c],   c < d.
+ * The normalisation between the aggregations of a deep network (Section 1's training step).
+ *   dtype: ISP_F32 | ISP_BF16 | ISP_F16, of X and Y; param_dtype: ISP_F32 or dtype, of weight and bias (d elements each; NULL: ones, zeros).
+ *     Everything is computed in 32 bits and rounded once.
+ *   ld* in elements, any value >= d, any alignment that fits an element.  n = 0 is valid.  X and Y must not overlap.
+ *   mean, rstd: fp32[n], written for the backward; each may be NULL.
+ */
+isp_status isp_layer_norm(const void* X, int64_t ldx, int64_t n, int32_t d, int dtype, const void* weight,
+                          const void* bias, int param_dtype, float eps, void* Y, int64_t ldy, float* mean,
+                          float* rstd, void* stream);
+
+/* Bytes of device workspace isp_layer_norm_backward needs when it is asked for dweight or dbias. */
+isp_status isp_layer_norm_backward_workspace(int64_t n, int32_t d, size_t* bytes);
+
+/*
+ * Gradients of the layer norm above for upstream gradient dY (of X's type): with h = (x - mean) rstd and g = dy weight,
+ *   dX = rstd (g - mean(g) - h mean(g h)),   dweight = sum over the rows of dy h,   dbias = sum over the rows of dy.
+ * mean and rstd are what the forward wrote.  dX, dweight and dbias (of param_dtype) may each be NULL: not wanted.
+ * The sums over the rows are formed in 32 bits per workgroup and in 64 across workgroups, in a fixed order.
+ * dX must not overlap X or dY.
+ *   workspace: 256-byte aligned, at least isp_layer_norm_backward_workspace bytes; used until the call's work on `stream` is done, nothing in it
+ *     needs clearing.  May be NULL when neither dweight nor dbias is wanted.
+ */
+isp_status isp_layer_norm_backward(const void* X, int64_t ldx, const void* dY, int64_t lddy, int64_t n, int32_t d,
+                                   int dtype, const void* weight, int param_dtype, const float* mean,
+                                   const float* rstd, void* dX, int64_t lddx, void* dweight, void* dbias,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace isp_label_logprob needs for this shape (0: none). */
+isp_status isp_label_logprob_workspace(int64_t n, int32_t n_classes, int32_t top, size_t* bytes);
+
+/*
+ * Log probabilities of given labels (a node classification's loss): per row i of the scores Z, with p = softmax(Z[i]),
+ *   logprob[i] = log p[labels[i]];  0 where labels[i] is outside [0, n_classes): the row has no label
+ *   entropy[i] = -sum_j p_j log p_j
+ *   top_index[i, k], top_logprob[i, k]: the class with the k-th largest score, k < top, and its log probability; equal scores in the order of
+ *     their classes, NaN above all numbers
+ *   stats[i] = (max of the row, log of the sum of exp(z - max)): what the backward needs, fp32 pairs
+ * A score of -inf leaves its class out (p = 0).  A row with nothing left: logprob and top_logprob -inf, entropy 0.  NaN or +inf in a row:
+ * its logprob, entropy and top_logprob are NaN.
+ *   dtype: of Z.  All other floating-point arrays are fp32.  labels: int64[n]; NULL only with logprob NULL.  logprob, entropy, stats, top_logprob and
+ *     top_index (int32, n x top, dense) may each be NULL: not wanted.  top: 0 ... min(n_classes, 64).  ldz as above.
+ *   workspace: 256-byte aligned, at least isp_label_logprob_workspace bytes (NULL when that is 0); nothing in it needs clearing.
+ */
+isp_status isp_label_logprob(const void* Z, int64_t ldz, int64_t n, int32_t n_classes, int dtype,
+                             const int64_t* labels, float* logprob, float* entropy, float* stats, int32_t top,
+                             float* top_logprob, int32_t* top_index, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
+/*
+ * Gradient of the above with respect to Z (of Z's type), for upstream gradients a of logprob and e of entropy (fp32[n]; each may be NULL: zero):
+ *   dZ[i, j] = a_i (1[j = label_i] - p_j) - e_i p_j (log p_j + entropy_i);  a_i counts as 0 where the row has no label.
+ * Rows with nothing left, and rows whose a_i and e_i are both 0, have gradient 0.  The top alternatives have no gradient.
+ * stats and entropy (the latter only with d_entropy) are what the forward wrote.  dZ must not overlap Z.
+ */
+isp_status isp_label_logprob_backward(const void* Z, int64_t ldz, int64_t n, int32_t n_classes, int dtype,
+                                      const int64_t* labels, const float* stats, const float* entropy,
+                                      const float* d_logprob, const float* d_entropy, void* dZ, int64_t lddz,
+                                      void* stream);
 
 /* Free the host-side handle and its cached transpose handle.  Never touches caller buffers.  NULL ok. */
 void isp_csr_destroy(isp_csr_t* A);

@@ -97,3 +97,57 @@ def fusedmm(graph: SparseGraph, X):
     if _recorder() is not None:
         return _Recorded.apply(lambda _, X: _b._nat.ag_fused(graph._native, X), None, X)
     return _b._nat.ag_fused(graph._native, X)
+
+
+class _RecordedRows(torch.autograd.Function):
+    """_Recorded for the operators below: any number of tensors, one output or several."""
+
+    @staticmethod
+    def forward(ctx, run, *tensors):
+        recorder = _recorder()
+        torch._C._set_tracing_state(None)
+        try:
+            with torch.enable_grad():
+                ctx.leaves = [t if t is None else t.detach().requires_grad_(need) for t, need in zip(tensors, ctx.needs_input_grad[1:])]
+                out = run(*ctx.leaves)
+        finally:
+            torch._C._set_tracing_state(recorder)
+        several = isinstance(out, tuple)
+        ctx.outputs = out if several else (out,)
+        first = next(t for t in tensors if t is not None)
+        results = tuple(first.new_empty(0, dtype=o.dtype) for o in ctx.outputs)  # (made while the recorder looks on)
+        torch._C._set_tracing_state(None)
+        try:
+            for r, o in zip(results, ctx.outputs):
+                r.set_(o.detach())
+        finally:
+            torch._C._set_tracing_state(recorder)
+        ctx.mark_non_differentiable(*(r for r, o in zip(results, ctx.outputs) if not o.requires_grad))
+        ctx.save_for_backward(*(t for t in tensors if t is not None))
+        return results if several else results[0]
+
+    @staticmethod
+    def backward(ctx, *grads):
+        ctx.saved_tensors
+        wanted = [t for t, need in zip(ctx.leaves, ctx.needs_input_grad[1:]) if need]
+        pairs = [(o, g) for o, g in zip(ctx.outputs, grads) if o.requires_grad]
+        got = iter(torch.autograd.grad([o for o, _ in pairs], wanted, [g for _, g in pairs], retain_graph=True))
+        return (None, *(next(got) if need else None for need in ctx.needs_input_grad[1:]))
+
+
+def layer_norm(X, weight=None, bias=None, eps: float = 1e-5):
+    """Differentiable layer norm over the rows of X (fp32, bf16 or fp16; weight and bias fp32 or of X's type)."""
+    nat = _b._native()
+    if _recorder() is not None:
+        return _RecordedRows.apply(lambda X, weight, bias: nat.ag_layer_norm(X, weight, bias, float(eps)), X, weight, bias)
+    return nat.ag_layer_norm(X, weight, bias, float(eps))
+
+
+def label_logprob(Z, labels, top: int = 0):
+    """(logprob, entropy) of the rows of scores Z (fp32, bf16 or fp16) for int64 labels, both fp32 and differentiable with respect to Z;
+    a label outside [0, classes) names no class: log probability 0, no gradient.  With top > 0 also the log probabilities and the
+    classes (int32) of that many best alternatives, which have no gradient: (logprob, entropy, top_logprob, top_index)."""
+    nat = _b._native()
+    if _recorder() is not None:
+        return _RecordedRows.apply(lambda Z, labels: nat.ag_label_logprob(Z, labels, int(top)), Z, labels)
+    return nat.ag_label_logprob(Z, labels, int(top))

@@ -20,7 +20,8 @@ EXPORTED_SYMBOLS = [
     "isp_csr_build_workspace", "isp_csr_build", "isp_csr_transpose_workspace", "isp_csr_transpose_cached",
     "isp_csr_values_changed", "isp_csr_alias_workspace", "isp_csr_alias", "isp_csr_export", "isp_csr_info", "isp_spmm",
     "isp_spmm_static_scratch", "isp_sddmm", "isp_fusedmm", "isp_fusedmm_backward",
-    "isp_spmm_reduce", "isp_spmm_reduce_backward", "isp_csr_destroy", "isp_last_error", "isp_version",
+    "isp_spmm_reduce", "isp_spmm_reduce_backward", "isp_layer_norm", "isp_layer_norm_backward_workspace",
+    "isp_layer_norm_backward", "isp_label_logprob_workspace", "isp_label_logprob", "isp_label_logprob_backward", "isp_csr_destroy", "isp_last_error", "isp_version",
 ]
 
 ISP_TRUSTED = 1
@@ -78,6 +79,12 @@ def load_library():
     lib.isp_fusedmm_backward.argtypes = [vp, vp, i64, vp, i64, i32, ctypes.c_int, vp, i64, vp]
     lib.isp_spmm_reduce.argtypes = [vp, vp, i64, i32, ctypes.c_int, vp, i64, vp, vp]
     lib.isp_spmm_reduce_backward.argtypes = [vp, vp, i64, i32, ctypes.c_int, vp, vp, i64, vp]
+    lib.isp_layer_norm.argtypes = [vp, i64, i64, i32, ctypes.c_int, vp, vp, ctypes.c_int, ctypes.c_float, vp, i64, vp, vp, vp]
+    lib.isp_layer_norm_backward_workspace.argtypes = [i64, i32, P(sz)]
+    lib.isp_layer_norm_backward.argtypes = [vp, i64, vp, i64, i64, i32, ctypes.c_int, vp, ctypes.c_int, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+    lib.isp_label_logprob_workspace.argtypes = [i64, i32, i32, P(sz)]
+    lib.isp_label_logprob.argtypes = [vp, i64, i64, i32, ctypes.c_int, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.isp_label_logprob_backward.argtypes = [vp, i64, i64, i32, ctypes.c_int, vp, vp, vp, vp, vp, vp, i64, vp]
     lib.isp_csr_destroy.argtypes = [vp]
     lib.isp_csr_destroy.restype = None
     for name in EXPORTED_SYMBOLS:
@@ -393,3 +400,69 @@ def spmm_reduce_backward(A: CSR, dY, dX, reduce: str, arg=None, *, stream=None):
     if st:
         _check(st)
     return dX
+
+
+def _call_workspace(workspace, nbytes, like, stream):
+    """The caller's workspace, or a fresh one whose memory belongs to the stream that the call runs on (None: none is needed)."""
+    if workspace is not None or nbytes == 0:
+        return workspace
+    import torch
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+
+
+def layer_norm(X, Y, weight=None, bias=None, *, eps=1e-5, mean=None, rstd=None, stream=None):
+    """isp_layer_norm: Y = layer norm of X's rows (fp32, bf16 or fp16; weight and bias fp32 or of that type).
+    mean, rstd: fp32 [rows], filled for layer_norm_backward."""
+    st = _native().layer_norm(X, Y, weight, bias, mean, rstd, float(eps), _raw(stream))
+    if st:
+        _check(st)
+    return Y
+
+
+def layer_norm_backward_workspace(n: int, d: int) -> int:
+    """isp_layer_norm_backward_workspace: bytes of device workspace for the sums over n rows of d columns."""
+    need = ctypes.c_size_t()
+    _check(load_library().isp_layer_norm_backward_workspace(int(n), int(d), ctypes.byref(need)))
+    return int(need.value)
+
+
+def layer_norm_backward(X, dY, dX, mean, rstd, weight=None, dweight=None, dbias=None, *, workspace=None, stream=None):
+    """isp_layer_norm_backward; dX, dweight, dbias: None where not wanted.  Returns dX."""
+    if (dweight is not None or dbias is not None) and X.dim() == 2 and X.shape[1] > 0:
+        workspace = _call_workspace(workspace, layer_norm_backward_workspace(*X.shape), X, stream)
+    st = _native().layer_norm_backward(X, dY, dX, mean, rstd, weight, dweight, dbias, workspace, _raw(stream))
+    if st:
+        _check(st)
+    return dX
+
+
+def label_logprob_workspace(n: int, n_classes: int, top: int = 0) -> int:
+    """isp_label_logprob_workspace: bytes of device workspace label_logprob needs for this shape (often 0)."""
+    need = ctypes.c_size_t()
+    _check(load_library().isp_label_logprob_workspace(int(n), int(n_classes), int(top), ctypes.byref(need)))
+    return int(need.value)
+
+
+def label_logprob(Z, labels, logprob, entropy=None, *, stats=None, top_logprob=None, top_index=None, workspace=None, stream=None):
+    """isp_label_logprob: logprob[i] = log softmax(Z[i])[labels[i]] (0 where the label names no class), the rows' entropy, and the top
+    alternatives, as many as top_logprob / top_index (int32) have columns.  stats: fp32 [rows, 2], filled for label_logprob_backward."""
+    if workspace is None and Z.dim() == 2 and Z.shape[1] > 0:
+        some = top_logprob if top_logprob is not None else top_index
+        top = some.shape[1] if some is not None and some.dim() == 2 else 0
+        if top <= Z.shape[1]:
+            workspace = _call_workspace(None, label_logprob_workspace(*Z.shape, top), Z, stream)
+    st = _native().label_logprob(Z, labels, logprob, entropy, stats, top_logprob, top_index, workspace, _raw(stream))
+    if st:
+        _check(st)
+    return logprob
+
+
+def label_logprob_backward(Z, labels, stats, d_logprob, dZ, *, entropy=None, d_entropy=None, stream=None):
+    """isp_label_logprob_backward: dZ from the gradients of logprob and entropy (None: zero)."""
+    st = _native().label_logprob_backward(Z, labels, stats, entropy, d_logprob, d_entropy, dZ, _raw(stream))
+    if st:
+        _check(st)
+    return dZ

@@ -330,6 +330,191 @@ PyObject* py_spmm_reduce_backward(PyObject*, PyObject* const* a, Py_ssize_t narg
   return call(c, w, [&](isp_csr_t* h, void* s) { return isp_spmm_reduce_backward(h, G.p, G.ld, (int32_t)G.d, red, arg, O.p, O.ld, s); });
 }
 
+// ---- operands of the operators that take half precision too ----------------------------------------------------------
+// Rows on the current device, fp32 or 16 bits, contiguous within a row.
+struct Mat {
+  void* p;
+  int64_t rows, d, ld;
+  int type;
+};
+int type_of(at::ScalarType t) { return t == at::kFloat ? ISP_F32 : t == at::kBFloat16 ? ISP_BF16 : t == at::kHalf ? ISP_F16 : -1; }
+bool is_here(const Tensor& t) { return t.is_cuda() && t.device().index() == c10::hip::current_device(); }
+const char* mat_of(const Tensor& t, Mat& o) {
+  if (t.dim() != 2) return "a dense operand has two dimensions";
+  if (!is_here(t)) return "a dense operand lives on the current GPU";
+  o.type = type_of(t.scalar_type());
+  if (o.type < 0) return "a dense operand is float32, bfloat16 or float16";
+  if (t.stride(1) != 1 && t.size(1) > 1) return "the rows of a dense operand are contiguous";
+  o.p = t.data_ptr();
+  o.rows = t.size(0);
+  o.d = t.size(1);
+  if (o.d > INT32_MAX) return "a dense operand has rows of at most 2^31 - 1 elements";
+  o.ld = o.rows > 1 ? t.stride(0) : std::max<int64_t>(t.stride(0), o.d);
+  return nullptr;
+}
+// A dense array of so many elements of one type (undefined: absent).
+const char* array_of(const Tensor& t, at::ScalarType type, int64_t n, void** o) {
+  *o = nullptr;
+  if (!t.defined()) return nullptr;
+  if (!is_here(t)) return "an array lives on the current GPU";
+  if (t.scalar_type() != type) return "an array has the wrong element type";
+  if (t.numel() != n) return "an array has the wrong number of elements";
+  if (!t.is_contiguous()) return "an array is contiguous";
+  *o = t.data_ptr();
+  return nullptr;
+}
+// What a caller handed over for it: None is an undefined tensor.
+bool maybe_tensor(PyObject* o, Tensor& t) {
+  if (o == Py_None) return true;
+  if (!is_tensor(o)) return false;
+  t = THPVariable_Unpack(o);
+  return true;
+}
+// The arguments' tensors, from a[i0] on.
+template <size_t N>
+bool tensors_of(PyObject* const* a, Tensor (&t)[N]) {
+  for (size_t i = 0; i < N; ++i)
+    if (!maybe_tensor(a[i], t[i])) return false;
+  return true;
+}
+#define ISP_REFUSE(what)                        \
+  if (const char* bad_ = (what)) return fail(bad_)
+#define ISP_REFUSE_IF(cond, what) \
+  if (cond) return fail(what)
+
+template <class F>
+PyObject* call_free(Where w, F&& f) {  // a library call without a handle
+  isp_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = f(w.s);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+// (workspaces: bytes on the current device)
+const char* bytes_of(const Tensor& t, void** p, size_t* n) {
+  *p = nullptr;
+  *n = 0;
+  if (!t.defined()) return nullptr;
+  if (!is_here(t) || t.scalar_type() != at::kByte || !t.is_contiguous()) return "a workspace is a contiguous uint8 tensor on the current GPU";
+  *p = t.data_ptr();
+  *n = t.numel();
+  return nullptr;
+}
+
+struct Norm {  // of the parameters
+  void *w = nullptr, *b = nullptr;
+  int type = ISP_F32;
+};
+const char* params_of(const Tensor& w, const Tensor& b, const Mat& X, Norm& o) {
+  const Tensor& any = w.defined() ? w : b;
+  if (!any.defined()) return nullptr;
+  o.type = type_of(any.scalar_type());
+  if (o.type != ISP_F32 && o.type != X.type) return "weight and bias are float32 or of the matrix's type";
+  if (const char* bad = array_of(w, any.scalar_type(), X.d, &o.w)) return bad;
+  return array_of(b, any.scalar_type(), X.d, &o.b);
+}
+
+// (X, Y, weight, bias, mean, rstd, eps, stream)
+PyObject* py_layer_norm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  ISP_ARGS(8)
+  Tensor t[6];
+  if (!is_tensor(a[0]) || !is_tensor(a[1]) || !tensors_of(a, t)) return nullptr;
+  Mat X, Y;
+  Norm P;
+  void *mean, *rstd;
+  ISP_REFUSE(mat_of(t[0], X));
+  ISP_REFUSE(mat_of(t[1], Y));
+  ISP_REFUSE_IF(Y.rows != X.rows || Y.d != X.d || Y.type != X.type, "X and Y have one shape and type");
+  ISP_REFUSE(params_of(t[2], t[3], X, P));
+  ISP_REFUSE(array_of(t[4], at::kFloat, X.rows, &mean));
+  ISP_REFUSE(array_of(t[5], at::kFloat, X.rows, &rstd));
+  const double eps = PyFloat_AsDouble(a[6]);
+  const Where w = stream_of(a[7]);
+  if (PyErr_Occurred()) return nullptr;
+  return call_free(w, [&](void* s) {
+    return isp_layer_norm(X.p, X.ld, X.rows, (int32_t)X.d, X.type, P.w, P.b, P.type, (float)eps, Y.p, Y.ld, (float*)mean, (float*)rstd, s);
+  });
+}
+
+// (X, dY, dX, mean, rstd, weight, dweight, dbias, workspace, stream)
+PyObject* py_layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  ISP_ARGS(10)
+  Tensor t[9];
+  if (!is_tensor(a[0]) || !is_tensor(a[1]) || !tensors_of(a, t)) return nullptr;
+  Mat X, G, O{nullptr, 0, 0, 0, 0};
+  Norm P, D;
+  void *mean, *rstd, *ws;
+  size_t bytes;
+  ISP_REFUSE(mat_of(t[0], X));
+  ISP_REFUSE(mat_of(t[1], G));
+  if (t[2].defined()) ISP_REFUSE(mat_of(t[2], O));
+  ISP_REFUSE_IF(G.rows != X.rows || G.d != X.d || G.type != X.type, "X and dY have one shape and type");
+  ISP_REFUSE_IF(t[2].defined() && (O.rows != X.rows || O.d != X.d || O.type != X.type), "X and dX have one shape and type");
+  ISP_REFUSE_IF(!t[3].defined() || !t[4].defined(), "the backward needs the forward's mean and rstd");
+  ISP_REFUSE(array_of(t[3], at::kFloat, X.rows, &mean));
+  ISP_REFUSE(array_of(t[4], at::kFloat, X.rows, &rstd));
+  ISP_REFUSE(params_of(t[5], Tensor(), X, P));
+  ISP_REFUSE(params_of(t[6], t[7], X, D));
+  ISP_REFUSE_IF(P.w && (D.w || D.b) && P.type != D.type, "the gradients of the parameters have the parameters' type");
+  ISP_REFUSE(bytes_of(t[8], &ws, &bytes));
+  const Where w = stream_of(a[9]);
+  if (PyErr_Occurred()) return nullptr;
+  return call_free(w, [&](void* s) {
+    return isp_layer_norm_backward(X.p, X.ld, G.p, G.ld, X.rows, (int32_t)X.d, X.type, P.w, P.w ? P.type : D.type, (const float*)mean, (const float*)rstd,
+                                   O.p, O.ld, D.w, D.b, ws, bytes, s);
+  });
+}
+
+// (Z, labels, logprob, entropy, stats, top_logprob, top_index, workspace, stream)
+PyObject* py_label_logprob(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  ISP_ARGS(9)
+  Tensor t[8];
+  if (!is_tensor(a[0]) || !tensors_of(a, t)) return nullptr;
+  Mat Z;
+  void *labels, *lp, *en, *stats, *tv, *ti, *ws;
+  size_t bytes;
+  ISP_REFUSE(mat_of(t[0], Z));
+  const Tensor& some = t[5].defined() ? t[5] : t[6];
+  ISP_REFUSE_IF(some.defined() && (some.dim() != 2 || some.size(1) > Z.d), "the alternatives have one row per row of scores, of no more than its classes");
+  const int64_t top = some.defined() ? some.size(1) : 0;
+  ISP_REFUSE(array_of(t[1], at::kLong, Z.rows, &labels));
+  ISP_REFUSE(array_of(t[2], at::kFloat, Z.rows, &lp));
+  ISP_REFUSE(array_of(t[3], at::kFloat, Z.rows, &en));
+  ISP_REFUSE(array_of(t[4], at::kFloat, 2 * Z.rows, &stats));
+  ISP_REFUSE(array_of(t[5], at::kFloat, Z.rows * top, &tv));
+  ISP_REFUSE(array_of(t[6], at::kInt, Z.rows * top, &ti));
+  ISP_REFUSE(bytes_of(t[7], &ws, &bytes));
+  const Where w = stream_of(a[8]);
+  if (PyErr_Occurred()) return nullptr;
+  return call_free(w, [&](void* s) {
+    return isp_label_logprob(Z.p, Z.ld, Z.rows, (int32_t)Z.d, Z.type, (const int64_t*)labels, (float*)lp, (float*)en, (float*)stats, (int32_t)top, (float*)tv,
+                             (int32_t*)ti, ws, bytes, s);
+  });
+}
+
+// (Z, labels, stats, entropy, d_logprob, d_entropy, dZ, stream)
+PyObject* py_label_logprob_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  ISP_ARGS(8)
+  Tensor t[7];
+  if (!is_tensor(a[0]) || !is_tensor(a[6]) || !tensors_of(a, t)) return nullptr;
+  Mat Z, O;
+  void *labels, *stats, *en, *da, *de;
+  ISP_REFUSE(mat_of(t[0], Z));
+  ISP_REFUSE(mat_of(t[6], O));
+  ISP_REFUSE_IF(O.rows != Z.rows || O.d != Z.d || O.type != Z.type, "Z and dZ have one shape and type");
+  ISP_REFUSE(array_of(t[1], at::kLong, Z.rows, &labels));
+  ISP_REFUSE(array_of(t[2], at::kFloat, 2 * Z.rows, &stats));
+  ISP_REFUSE(array_of(t[3], at::kFloat, Z.rows, &en));
+  ISP_REFUSE(array_of(t[4], at::kFloat, Z.rows, &da));
+  ISP_REFUSE(array_of(t[5], at::kFloat, Z.rows, &de));
+  const Where w = stream_of(a[7]);
+  if (PyErr_Occurred()) return nullptr;
+  return call_free(w, [&](void* s) {
+    return isp_label_logprob_backward(Z.p, Z.ld, Z.rows, (int32_t)Z.d, Z.type, (const int64_t*)labels, (const float*)stats, (const float*)en, (const float*)da,
+                                      (const float*)de, O.p, O.ld, s);
+  });
+}
+
 // ---- autograd -------------------------------------------------------------------------------------------------
 // The same operations as nodes of torch's graph.  The backward touches the interpreter only when a transpose has to
 // be built or a call fails.  (4,096 rows, 32 columns, forward + backward: 112 -> 44 us of host time; a multiplication by
@@ -613,6 +798,193 @@ PyObject* py_ag_fused(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- the row-wise operators' nodes -------------------------------------------------------------------------------------
+Mat mat(const Tensor& t) {
+  Mat o;
+  if (const char* bad = mat_of(t, o)) assertion(bad);
+  return o;
+}
+void* array(const Tensor& t, at::ScalarType type, int64_t n) {
+  void* p;
+  if (const char* bad = array_of(t, type, n, &p)) assertion(bad);
+  return p;
+}
+Norm params(const Tensor& w, const Tensor& b, const Mat& X) {
+  Norm o;
+  if (const char* bad = params_of(w, b, X, o)) assertion(bad);
+  return o;
+}
+Tensor rows_of(const Tensor& t) { return t.dim() == 2 && t.stride(1) == 1 && (t.size(0) < 2 || t.stride(0) >= t.size(1)) ? t : t.contiguous(); }
+Tensor floats_like(const Tensor& t, at::IntArrayRef shape) { return at::empty(shape, t.options().dtype(at::kFloat).requires_grad(false)); }
+Tensor workspace_like(const Tensor& t, size_t bytes) { return at::empty({(int64_t)bytes}, t.options().dtype(at::kByte).requires_grad(false)); }
+using torch::autograd::SavedVariable;
+
+struct LayerNormBackward : torch::autograd::Node {
+  SavedVariable X, weight;
+  Tensor mean, rstd;
+  bool bias = false;
+  at::ScalarType param = at::kFloat;
+  std::string name() const override { return "IspLayerNormBackward"; }
+  void release_variables() override {
+    X.reset_data();
+    weight.reset_data();
+    mean.reset();
+    rstd.reset();
+  }
+  variable_list apply(variable_list&& grads) override {
+    variable_list out(3);
+    if (!grads[0].defined()) return out;
+    at::NoGradGuard no_grad;
+    const Tensor x = X.unpack(), w = weight.unpack(), dY = rows_of(grads[0]);
+    const Mat M = mat(x), G = mat(dY);
+    const Norm P = params(w, Tensor(), M);
+    Mat O{nullptr, 0, 0, 0, 0};
+    if (task_should_compute_output(0)) {
+      out[0] = at::empty({M.rows, M.d}, x.options().requires_grad(false));
+      O = mat(out[0]);
+    }
+    const auto like = x.options().dtype(param).requires_grad(false);
+    if (P.w && task_should_compute_output(1)) out[1] = at::empty({M.d}, like);
+    if (bias && task_should_compute_output(2)) out[2] = at::empty({M.d}, like);
+    size_t bytes = 0;
+    Tensor ws;
+    if (out[1].defined() || out[2].defined()) {
+      check(isp_layer_norm_backward_workspace(M.rows, (int32_t)M.d, &bytes));
+      ws = workspace_like(x, bytes);
+    }
+    check(isp_layer_norm_backward(M.p, M.ld, G.p, G.ld, M.rows, (int32_t)M.d, M.type, P.w, type_of(param), mean.data_ptr<float>(), rstd.data_ptr<float>(),
+                                  O.p, O.ld, out[1].defined() ? out[1].data_ptr() : nullptr, out[2].defined() ? out[2].data_ptr() : nullptr,
+                                  ws.defined() ? ws.data_ptr() : nullptr, bytes, here().s));
+    return out;
+  }
+};
+
+// (X, weight or None, bias or None, eps) -> Y
+PyObject* py_ag_layer_norm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  ISP_ARGS(4)
+  Tensor t[3];
+  if (!is_tensor(a[0]) || !tensors_of(a, t)) return nullptr;
+  const double eps = PyFloat_AsDouble(a[3]);
+  if (PyErr_Occurred()) return nullptr;
+  for (const Tensor& v : t)
+    if (!no_tangent(v)) return nullptr;
+  Tensor Y;
+  {
+    pybind11::gil_scoped_release release;
+    Tensor x, w, b, mean, rstd;
+    const bool grad = torch::autograd::compute_requires_grad(t[0], t[1], t[2]);
+    Norm P;
+    {
+      at::NoGradGuard no_grad;
+      x = rows_of(t[0]);
+      if (t[1].defined()) w = t[1].contiguous();
+      if (t[2].defined()) b = t[2].contiguous();
+      const Mat X = mat(x);
+      P = params(w, b, X);
+      Y = at::empty({X.rows, X.d}, x.options().requires_grad(false));
+      const Mat O = mat(Y);
+      if (grad) {
+        mean = floats_like(x, {X.rows});
+        rstd = floats_like(x, {X.rows});
+      }
+      check(isp_layer_norm(X.p, X.ld, X.rows, (int32_t)X.d, X.type, P.w, P.b, P.type, (float)eps, O.p, O.ld, grad ? mean.data_ptr<float>() : nullptr,
+                           grad ? rstd.data_ptr<float>() : nullptr, here().s));
+    }
+    if (grad) {
+      auto node = std::shared_ptr<LayerNormBackward>(new LayerNormBackward(), torch::autograd::deleteNode);
+      node->set_next_edges(torch::autograd::collect_next_edges(t[0], t[1], t[2]));
+      node->X = SavedVariable(x, false);
+      if (w.defined()) node->weight = SavedVariable(w, false);
+      node->mean = mean;
+      node->rstd = rstd;
+      node->bias = b.defined();
+      node->param = P.type == ISP_F32 ? at::kFloat : x.scalar_type();
+      torch::autograd::set_history(Y, node);
+    }
+  }
+  return THPVariable_Wrap(Y);
+  END_HANDLE_TH_ERRORS
+}
+
+struct LabelLogprobBackward : torch::autograd::Node {
+  SavedVariable Z, labels, entropy;
+  Tensor stats;
+  std::string name() const override { return "IspLabelLogprobBackward"; }
+  void release_variables() override {
+    Z.reset_data();
+    labels.reset_data();
+    entropy.reset_data();
+    stats.reset();
+  }
+  variable_list apply(variable_list&& grads) override {
+    variable_list out(1);
+    if (!grads[0].defined() && !grads[1].defined()) return out;
+    at::NoGradGuard no_grad;
+    const Tensor z = Z.unpack(), y = labels.unpack(), e = entropy.unpack(shared_from_this());
+    const Mat M = mat(z);
+    const Tensor da = grads[0].defined() ? grads[0].contiguous() : Tensor(), de = grads[1].defined() ? grads[1].contiguous() : Tensor();
+    out[0] = at::empty({M.rows, M.d}, z.options().requires_grad(false));
+    const Mat O = mat(out[0]);
+    check(isp_label_logprob_backward(M.p, M.ld, M.rows, (int32_t)M.d, M.type, static_cast<const int64_t*>(array(y, at::kLong, M.rows)), stats.data_ptr<float>(),
+                                     static_cast<const float*>(array(e, at::kFloat, M.rows)), static_cast<const float*>(array(da, at::kFloat, M.rows)),
+                                     static_cast<const float*>(array(de, at::kFloat, M.rows)), O.p, O.ld, here().s));
+    return out;
+  }
+};
+
+// (Z, labels, top) -> (logprob, entropy) or, with top > 0, (logprob, entropy, top_logprob, top_index)
+PyObject* py_ag_label_logprob(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  ISP_ARGS(3)
+  if (!is_tensor(a[0]) || !is_tensor(a[1])) return nullptr;
+  const Tensor Z = THPVariable_Unpack(a[0]), labels = THPVariable_Unpack(a[1]);
+  const long top = PyLong_AsLong(a[2]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!no_tangent(Z)) return nullptr;
+  Tensor lp, en, tv, ti;
+  {
+    pybind11::gil_scoped_release release;
+    const bool grad = torch::autograd::compute_requires_grad(Z);
+    Tensor z, y, stats;
+    {
+      at::NoGradGuard no_grad;
+      z = rows_of(Z);
+      y = labels.contiguous();
+      const Mat M = mat(z);
+      if (top < 0 || top > M.d) assertion("top is not in [0, classes]");
+      const auto* L = static_cast<const int64_t*>(array(y, at::kLong, M.rows));
+      lp = floats_like(z, {M.rows});
+      en = floats_like(z, {M.rows});
+      if (grad) stats = floats_like(z, {M.rows, 2});
+      if (top > 0) {
+        tv = floats_like(z, {M.rows, top});
+        ti = at::empty({M.rows, top}, tv.options().dtype(at::kInt));
+      }
+      size_t bytes = 0;
+      check(isp_label_logprob_workspace(M.rows, (int32_t)M.d, (int32_t)top, &bytes));
+      Tensor ws;
+      if (bytes) ws = workspace_like(z, bytes);
+      check(isp_label_logprob(M.p, M.ld, M.rows, (int32_t)M.d, M.type, L, lp.data_ptr<float>(), en.data_ptr<float>(), grad ? stats.data_ptr<float>() : nullptr,
+                              (int32_t)top, top > 0 ? tv.data_ptr<float>() : nullptr, top > 0 ? ti.data_ptr<int32_t>() : nullptr,
+                              bytes ? ws.data_ptr() : nullptr, bytes, here().s));
+    }
+    if (grad) {
+      auto node = std::shared_ptr<LabelLogprobBackward>(new LabelLogprobBackward(), torch::autograd::deleteNode);
+      node->set_next_edges(torch::autograd::collect_next_edges(Z));
+      node->Z = SavedVariable(z, false);
+      node->labels = SavedVariable(y, false);
+      node->stats = stats;
+      torch::autograd::set_history(lp, node);
+      torch::autograd::set_history(en, node);
+      node->entropy = SavedVariable(en, true);
+    }
+  }
+  return top > 0 ? Py_BuildValue("(NNNN)", THPVariable_Wrap(lp), THPVariable_Wrap(en), THPVariable_Wrap(tv), THPVariable_Wrap(ti))
+                 : Py_BuildValue("(NN)", THPVariable_Wrap(lp), THPVariable_Wrap(en));
+  END_HANDLE_TH_ERRORS
+}
+
 // (binding._check, binding.csr_transpose_cached)
 PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   ISP_ARGS(2)
@@ -649,6 +1021,12 @@ PyMethodDef methods[] = {
     ISP_DEF("fusedmm_backward", py_fusedmm_backward),
     ISP_DEF("spmm_reduce", py_spmm_reduce),
     ISP_DEF("spmm_reduce_backward", py_spmm_reduce_backward),
+    ISP_DEF("layer_norm", py_layer_norm),
+    ISP_DEF("layer_norm_backward", py_layer_norm_backward),
+    ISP_DEF("label_logprob", py_label_logprob),
+    ISP_DEF("label_logprob_backward", py_label_logprob_backward),
+    ISP_DEF("ag_layer_norm", py_ag_layer_norm),
+    ISP_DEF("ag_label_logprob", py_ag_label_logprob),
     ISP_DEF("graph", py_graph),
     ISP_DEF("graph_sync", py_graph_sync),
     ISP_DEF("ag_spmm", py_ag_spmm),
