@@ -77,6 +77,8 @@ typedef enum {
 #define ISP_TRUSTED 1u /* skip the structural validation pass (the caller vouches for the CSR) */
 /* flags of isp_sddmm */
 #define ISP_SCALE_BY_A 1u /* multiply each dot product by the entry's value */
+/* flags of isp_attention / isp_attention_backward */
+#define ISP_BIAS_BY_A 1u /* add the entry's value to its score */
 /* op of isp_fusedmm / isp_fusedmm_backward: the edge function s = f(z) applied to z = <x_i, x_j> */
 #define ISP_OP_SIGMOID 0 /* f(z) = 1 / (1 + exp(-z)) */
 #define ISP_OP_DOT 1     /* f(z) = z */
@@ -305,6 +307,47 @@ isp_status isp_spmm_reduce(const isp_csr_t* A, const float* X, int64_t ldx, int3
  */
 isp_status isp_spmm_reduce_backward(isp_csr_t* A, const float* dY, int64_t lddy, int32_t d, int reduce,
                                     const int32_t* arg, float* dX, int64_t lddx, void* stream);
+
+/* Bytes of device workspace isp_attention needs on A (0: none): the partial rows of the segments of split rows. */
+isp_status isp_attention_workspace(const isp_csr_t* A, int32_t heads, int32_t head_dim, size_t* bytes);
+
+/*
+ * Attention over the stored entries of A: FusedMM (Section 1(a)) with the softmax over each row's entries as its edge function, and
+ * queries, keys and values of their own.  Per query head h, with key head g = h / (heads / kv_heads) and p = (i, j) the entries of row i:
+ *   s_p = scale <Q[i, h], K[j, g]> (+ values[p] with ISP_BIAS_BY_A),   P = softmax of s over the row's entries,   Y[i, h] = sum_p P_p V[j, g].
+ * A says which keys a query sees: a graph, a batch of graphs of different sizes (block diagonal), a causal or any other pattern.  Repeated columns
+ * are entries of their own.  Without ISP_BIAS_BY_A the values are not looked at.  A bias of -inf masks its entry, whatever K and V hold there.
+ * Rows without entries, or with masked ones only: Y = 0.
+ *   Q, Y: n_rows x (heads * head_dim), K, V: n_cols x (kv_heads * head_dim), row-major, head after head; any ld (rows less than 4 GB apart) and
+ *     any alignment that fits an element; dtype: ISP_F32 | ISP_BF16 | ISP_F16, of all four.  Scores, sums and products with P are held in 32 bits,
+ *     Y is rounded once.  heads a multiple of kv_heads (at most 4096), head_dim <= 256.  Y must not overlap an operand.
+ *   stats: fp32, n_rows x heads x 2, written for the backward: a reference m for the row's scores and the sum of exp(s - m).  May be NULL.
+ *   workspace: 256-byte aligned, at least isp_attention_workspace bytes; used until the call's work on `stream` is done, nothing in it needs clearing.
+ * Nothing of the handle's own scratch is used: calls on one handle may overlap, with a workspace each.
+ */
+isp_status isp_attention(const isp_csr_t* A, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V,
+                         int64_t ldv, int32_t heads, int32_t kv_heads, int32_t head_dim, float scale,
+                         unsigned flags, int dtype, void* Y, int64_t ldy, float* stats, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace isp_attention_backward needs on A as it is (with its cached transpose, if that is there). */
+isp_status isp_attention_backward_workspace(const isp_csr_t* A, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                            size_t* bytes);
+
+/*
+ * Gradients of the attention above for upstream gradient dY: with t_p = <dY[i, h], V[j, g]>, D_i = sum_{p in row i} P_p t_p and dS_p = P_p (t_p - D_i)
+ *   dQ[i, h] = scale sum_{p in row i} dS_p K[j, g],
+ *   dK[j, g] = scale sum over the query heads of g and the entries p in column j of dS_p Q[i, h],   dV[j, g] = the same sum of P_p dY[i, h].
+ * The column sums run over the rows of the cached transpose (Section 3.3), so isp_csr_transpose_cached(A) must have succeeded before - otherwise
+ * ISP_EINVAL - unless dK and dV are NULL.  dQ, or dK and dV together, may be NULL: not wanted.  All of dtype, overwritten.
+ * stats is what the forward wrote, with the same operands, scale, flags and values.  The scores are computed again, not read back.
+ * There is no gradient with respect to the values.
+ */
+isp_status isp_attention_backward(const isp_csr_t* A, const void* Q, int64_t ldq, const void* K, int64_t ldk,
+                                  const void* V, int64_t ldv, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                  float scale, unsigned flags, int dtype, const float* stats, const void* dY,
+                                  int64_t lddy, void* dQ, int64_t lddq, void* dK, int64_t lddk, void* dV,
+                                  int64_t lddv, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Layer norm over the rows of a dense matrix: with the row's mean and rstd = (mean of (x - mean)^2 + eps)^-1/2,

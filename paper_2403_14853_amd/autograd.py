@@ -151,3 +151,17 @@ def label_logprob(Z, labels, top: int = 0):
     if _recorder() is not None:
         return _RecordedRows.apply(lambda Z, labels: nat.ag_label_logprob(Z, labels, int(top)), Z, labels)
     return nat.ag_label_logprob(Z, labels, int(top))
+
+
+def attention(graph: SparseGraph, Q, K, V, heads: int, kv_heads=None, *, scale=None, bias: bool = False):
+    """Differentiable attention over the graph's entries (with respect to Q, K and V): per head, Y[i] = sum over row i's entries (i, j) of
+    softmax(scale <Q[i], K[j]> (+ the entry's value with bias=True)) V[j].  Q [rows, heads * c], K, V [columns, kv_heads * c], fp32, bf16 or
+    fp16; heads is a multiple of kv_heads (default: heads); scale: c ** -0.5 unless given."""
+    if bias and graph.values is not None and graph.values.requires_grad:
+        raise NotImplementedError("the attention has no gradient with respect to the edge values")
+    kv_heads = heads if kv_heads is None else kv_heads
+    scale = None if scale is None else float(scale)
+    call = lambda Q, K, V: _b._nat.ag_attention(graph._native, Q, K, V, int(heads), int(kv_heads), scale, _b.ISP_BIAS_BY_A if bias else 0)
+    if _recorder() is not None:
+        return _RecordedRows.apply(call, Q, K, V)
+    return call(Q, K, V)

@@ -20,12 +20,14 @@ EXPORTED_SYMBOLS = [
     "isp_csr_build_workspace", "isp_csr_build", "isp_csr_transpose_workspace", "isp_csr_transpose_cached",
     "isp_csr_values_changed", "isp_csr_alias_workspace", "isp_csr_alias", "isp_csr_export", "isp_csr_info", "isp_spmm",
     "isp_spmm_static_scratch", "isp_sddmm", "isp_fusedmm", "isp_fusedmm_backward",
-    "isp_spmm_reduce", "isp_spmm_reduce_backward", "isp_layer_norm", "isp_layer_norm_backward_workspace",
+    "isp_spmm_reduce", "isp_spmm_reduce_backward", "isp_attention_workspace", "isp_attention",
+    "isp_attention_backward_workspace", "isp_attention_backward", "isp_layer_norm", "isp_layer_norm_backward_workspace",
     "isp_layer_norm_backward", "isp_label_logprob_workspace", "isp_label_logprob", "isp_label_logprob_backward", "isp_csr_destroy", "isp_last_error", "isp_version",
 ]
 
 ISP_TRUSTED = 1
 ISP_SCALE_BY_A = 1
+ISP_BIAS_BY_A = 1
 ISP_OP_SIGMOID, ISP_OP_DOT, ISP_OP_ONE = 0, 1, 2
 EDGE_OPS = {"sigmoid": 0, "dot": 1, "one": 2}
 _STATUS = {0: "ISP_OK", 1: "ISP_EINVAL", 2: "ISP_EBADCSR", 3: "ISP_ENOMEM", 4: "ISP_EHIP", 5: "ISP_EUNSUPPORTED"}
@@ -79,6 +81,11 @@ def load_library():
     lib.isp_fusedmm_backward.argtypes = [vp, vp, i64, vp, i64, i32, ctypes.c_int, vp, i64, vp]
     lib.isp_spmm_reduce.argtypes = [vp, vp, i64, i32, ctypes.c_int, vp, i64, vp, vp]
     lib.isp_spmm_reduce_backward.argtypes = [vp, vp, i64, i32, ctypes.c_int, vp, vp, i64, vp]
+    heads = [vp, vp, i64, vp, i64, vp, i64, i32, i32, i32, ctypes.c_float, u32, ctypes.c_int]
+    lib.isp_attention_workspace.argtypes = [vp, i32, i32, P(sz)]
+    lib.isp_attention.argtypes = heads + [vp, i64, vp, vp, sz, vp]
+    lib.isp_attention_backward_workspace.argtypes = [vp, i32, i32, i32, P(sz)]
+    lib.isp_attention_backward.argtypes = heads + [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, sz, vp]
     lib.isp_layer_norm.argtypes = [vp, i64, i64, i32, ctypes.c_int, vp, vp, ctypes.c_int, ctypes.c_float, vp, i64, vp, vp, vp]
     lib.isp_layer_norm_backward_workspace.argtypes = [i64, i32, P(sz)]
     lib.isp_layer_norm_backward.argtypes = [vp, i64, vp, i64, i64, i32, ctypes.c_int, vp, ctypes.c_int, vp, vp, vp, i64, vp, vp, vp, sz, vp]
@@ -466,3 +473,52 @@ def label_logprob_backward(Z, labels, stats, d_logprob, dZ, *, entropy=None, d_e
     if st:
         _check(st)
     return dZ
+
+
+def attention_workspace(A: CSR, heads: int, head_dim: int) -> int:
+    """isp_attention_workspace: bytes of device workspace a forward call on A needs."""
+    need = ctypes.c_size_t()
+    _check(load_library().isp_attention_workspace(A._h, int(heads), int(head_dim), ctypes.byref(need)))
+    return int(need.value)
+
+
+def attention_backward_workspace(A: CSR, heads: int, kv_heads: int, head_dim: int) -> int:
+    """isp_attention_backward_workspace: bytes of device workspace a backward call on A needs (its cached transpose included)."""
+    need = ctypes.c_size_t()
+    _check(load_library().isp_attention_backward_workspace(A._h, int(heads), int(kv_heads), int(head_dim), ctypes.byref(need)))
+    return int(need.value)
+
+
+def _head_dim(Q, heads: int) -> int:
+    """Columns of a head; 0 where Q does not have `heads` of them (which the call itself refuses)."""
+    return Q.shape[1] // heads if Q.dim() == 2 and heads > 0 and Q.shape[1] % heads == 0 else 0
+
+
+def attention(A: CSR, Q, K, V, Y, heads: int, kv_heads=None, *, scale=None, bias=False, stats=None, workspace=None, stream=None):
+    """isp_attention: Y[i] = softmax over row i's entries of scale <Q[i], K[j]> (+ the entries' values with bias=True), times V[j], per head.
+    Q, Y [rows, heads * c], K, V [columns, kv_heads * c], fp32, bf16 or fp16; scale: c ** -0.5 unless given.
+    stats: fp32 [rows, heads, 2], filled for attention_backward."""
+    heads = int(heads)
+    kv_heads = heads if kv_heads is None else int(kv_heads)
+    c = _head_dim(Q, heads)
+    if workspace is None and c:
+        workspace = _call_workspace(None, attention_workspace(A, heads, c), Q, stream)
+    st = _nat.attention(A._cell, Q, K, V, Y, stats, workspace, heads, kv_heads, float(scale if scale is not None else max(c, 1) ** -0.5),
+                        ISP_BIAS_BY_A if bias else 0, _raw(stream))
+    if st:
+        _check(st)
+    return Y
+
+
+def attention_backward(A: CSR, Q, K, V, stats, dY, dQ, dK, dV, heads: int, kv_heads=None, *, scale=None, bias=False, workspace=None, stream=None):
+    """isp_attention_backward (needs csr_transpose_cached(A) first, unless dK and dV are None: not wanted, as dQ may be).  Returns (dQ, dK, dV)."""
+    heads = int(heads)
+    kv_heads = heads if kv_heads is None else int(kv_heads)
+    c = _head_dim(Q, heads)
+    if workspace is None and c and kv_heads > 0 and heads % kv_heads == 0:
+        workspace = _call_workspace(None, attention_backward_workspace(A, heads, kv_heads, c), Q, stream)
+    st = _nat.attention_backward(A._cell, Q, K, V, stats, dY, dQ, dK, dV, workspace, heads, kv_heads,
+                                 float(scale if scale is not None else max(c, 1) ** -0.5), ISP_BIAS_BY_A if bias else 0, _raw(stream))
+    if st:
+        _check(st)
+    return dQ, dK, dV

@@ -12,7 +12,8 @@ LIB = os.path.join(HERE, "libisp.so")
 SOURCES = ["isp_api.hip", "scan.hip", "csr_build.hip", "transpose.hip", "spmm.hip", "sddmm.hip", "fusedmm.hip",
            "fused_fwd.hip", "fused_bwd_row.hip", "fused_bwd_col.hip", "fused_bwd_mirror.hip",
            "spmm_reduce.hip", "static_scratch.hip", "alias.hip",
-           "rowwise.hip", "layer_norm.hip", "label_logprob.hip"]
+           "rowwise.hip", "layer_norm.hip", "label_logprob.hip", "attention.hip", "attention_f32.hip", "attention_bf16.hip",
+           "attention_f16.hip"]
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     # keep the compiler from forming packed-fp32 VALU ops out of scalar float code

@@ -1,0 +1,752 @@
+// Attention over the stored entries of a CSR matrix (gfx950, wave64): the three passes' kernels, instantiated per element type in attention_*.hip.
+//   forward   s_p = scale <q_i, k_j> + bias_p,  P = softmax over row i's entries,  y_i = sum_p P_p v_j           (p = (i, j))
+//   backward  t_p = <dy_i, v_j>,  D_i = sum_p P_p t_p,  dS_p = P_p (t_p - D_i)
+//             rows of A:    dq_i = scale sum_p dS_p k_j = scale (sum_p P_p t_p k_j - D_i sum_p P_p k_j)
+//             rows of A^T:  dk_j = scale sum_p dS_p q_i,   dv_j = sum_p P_p dy_i
+// with `heads` query heads on `kv_heads` key heads: query head h reads key head h / R, R = heads / kv_heads.
+//
+// The work items and runs of run_stream.h.  A lane has W consecutive columns of one key head (and of RQ of the R query heads that read
+// it); lph lanes span a head, a group of LPG lanes LPG / lph heads, and G = 64 / LPG groups stream their runs of entries side by side.  Scores are sums over
+// lph lanes; each gathered row of K and V serves the group's heads at once, and RQ query heads share it in registers.  Heads that don't fit
+// the group are other workgroups' (blockIdx.y), query heads beyond RQ too (blockIdx.z).  No score is ever written: the backward computes them again.
+//
+// Softmax in one pass: a row's (m, l, y) are a reference for its scores, the sum of exp(s - m) and of exp(s - m) v.  m is the
+// first score, and moves only to a score that is above it by more than ATT_SLACK: the sums stay far from overflow and almost no step has to
+// rescale.  Parts of a row that a run boundary cuts, or a split row's segments, are joined by their references, in a fixed order.
+// In the backward the rows' pass forms D beside dq's two sums, so that y, which has been rounded, is not needed, and leaves it to the
+// columns' pass.
+// Entries whose bias is -inf count for nothing, whatever their operands hold; a row without others has y = 0, l = 0.
+// Everything is held in 32 bits; outputs are rounded once.
+#pragma once
+#include "attention_args.h"
+#include "elem.h"
+#include "run_stream.h"
+
+namespace {
+using namespace isp_dev;
+
+constexpr float ATT_SLACK = 8.f;
+
+// Where a lane works.
+template <int W, bool TINY>
+struct att_lane {
+  int lph;    // lanes per head
+  int hk;     // key head (of a lane without one: the last)
+  int c;      // first column of its vector within the head: the last vector of a head moves back to end with it
+  int lo, hi; // elements [lo, hi) of the vector are its own (a moved-back vector's leading ones belong to the vector before)
+  bool live, first;  // first: has the head's first column
+  __device__ __forceinline__ att_lane(const att_args& a, int q, int hb) {
+    lph = a.lph;
+    const int h = (int)blockIdx.y * hb + q / lph, c0 = (q % lph) * W;
+    live = h < a.kv_heads && c0 < a.dh;
+    hk = h < a.kv_heads ? h : a.kv_heads - 1;
+    c = TINY ? 0 : c0 + W <= a.dh ? c0 : a.dh - W;
+    lo = live ? c0 - c : W;
+    hi = TINY ? a.dh : W;
+    first = live && c0 == 0;
+  }
+  __device__ __forceinline__ int col(int head, int dh) const { return head * dh + c; }
+};
+
+// A lane's vector as it lies in memory.
+template <class T, int W, bool TINY>
+__device__ __forceinline__ raw_t<T, W> att_load(const T* p, int dh) {
+  if constexpr (TINY) {  // (heads of fewer than W columns: what lies behind may not be ours)
+    raw_t<T, W> v;
+#pragma unroll
+    for (int j = 0; j < W; ++j) v[j] = p[j < dh ? j : dh - 1];
+    return v;
+  } else {
+    return load_raw<T, W>(p);
+  }
+}
+template <class T, int W, bool TINY>
+__device__ __forceinline__ void att_store(T* p, int dh, const float (&o)[W]) {
+  if constexpr (TINY) {
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      if (j < dh) p[j] = (T)o[j];
+  } else {
+    store_raw<T, W>(p, o);
+  }
+}
+
+// N sums over lph lanes (lph: a power of two, at most LPG; wave-uniform).
+template <int LPG, int N>
+__device__ __forceinline__ void att_sums(float (&v)[N], int lph) {
+#define ISP_STAGE(n, expr)                           \
+  if (LPG >= n && lph >= n) {                        \
+    _Pragma("unroll") for (int k = 0; k < N; ++k) v[k] += expr; \
+  }
+  ISP_STAGE(2, dpp_of<DPP_XOR1>(v[k]))
+  ISP_STAGE(4, dpp_of<DPP_XOR2>(v[k]))
+  ISP_STAGE(8, dpp_of<DPP_HALF_MIRROR>(v[k]))
+  ISP_STAGE(16, dpp_of<DPP_ROR8>(v[k]))
+  ISP_STAGE(32, __shfl_xor(v[k], 16))
+  ISP_STAGE(64, __shfl_xor(v[k], 32))
+#undef ISP_STAGE
+}
+
+template <int W>
+__device__ __forceinline__ float att_dot(const float (&a)[W], const float (&b)[W]) {
+  float s = a[0] * b[0];
+#pragma unroll
+  for (int j = 1; j < W; ++j) s = fmaf(a[j], b[j], s);
+  return s;
+}
+// A lane's elements of a row operand, times f; those that are not its own as zero, so that they add nothing to a dot product.
+template <class T, int W, bool TINY>
+__device__ __forceinline__ void att_own(const raw_t<T, W>& r, const att_lane<W, TINY>& ln, float f, float (&o)[W]) {
+  to_float<T, W>(r, o);
+#pragma unroll
+  for (int j = 0; j < W; ++j) o[j] = j >= ln.lo && j < ln.hi ? o[j] * f : 0.f;
+}
+
+template <class T>
+__device__ __forceinline__ const T* att_row(const void* base, uint32_t row, uint32_t pitch) {  // (pitch in bytes)
+  return reinterpret_cast<const T*>(static_cast<const char*>(base) + (uint64_t)row * pitch);
+}
+
+// ---- forward -------------------------------------------------------------------------------------------------------
+template <class T_, int W_, int RQ_, bool TINY_>
+struct att_fwd {
+  using T = T_;
+  static constexpr int W = W_, RQ = RQ_, RING = RQ == 1 ? 4 : 2, PARTS = RQ;
+  static constexpr bool TINY = TINY_;
+  using lane_t = att_lane<W, TINY>;
+  struct gathered { raw_t<T, W> k, v; };
+  struct requested { raw_t<T, W> q[RQ]; };
+  struct row_t { float q[RQ][W]; };
+  struct part { float y[W], m, l; };  // of a query head
+
+  static __device__ __forceinline__ int head(const att_args& a, const lane_t& ln, int r) { return ln.hk * a.group + (int)blockIdx.z * RQ + r; }
+  static __device__ __forceinline__ void clear(part& s) {
+    s.m = NEG_INF;
+    s.l = 0.f;
+#pragma unroll
+    for (int j = 0; j < W; ++j) s.y[j] = 0.f;
+  }
+  static __device__ __forceinline__ void gather(const att_args& a, const lane_t& ln, int col, gathered& o) {
+    const int at = ln.col(ln.hk, a.dh);
+    o.k = att_load<T, W, TINY>(att_row<T>(a.k, col, a.pk) + at, a.dh);
+    o.v = att_load<T, W, TINY>(att_row<T>(a.v, col, a.pv) + at, a.dh);
+  }
+  // (other steps than a row's first read one and the same line, which keeps the number of loads per step fixed)
+  static __device__ __forceinline__ void request(const att_args& a, const lane_t& ln, int row, bool first, requested& o) {
+    const T* p = att_row<T>(a.q, first ? row : 0, a.pq);
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) o.q[r] = att_load<T, W, TINY>(p + (first ? ln.col(head(a, ln, r), a.dh) : 0), a.dh);
+  }
+  static __device__ __forceinline__ void row(const att_args& a, const lane_t& ln, const requested& o, row_t& w) {
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) att_own<T, W, TINY>(o.q[r], ln, a.scale, w.q[r]);
+  }
+  template <int LPG>
+  static __device__ __forceinline__ void edge(const att_args& a, const lane_t& ln, float bias, const gathered& g, const row_t& w, part (&s)[PARTS]) {
+    float k[W], v[W], z[RQ];
+    to_float<T, W>(g.k, k);
+    to_float<T, W>(g.v, v);
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) z[r] = att_dot<W>(w.q[r], k);
+    att_sums<LPG, RQ>(z, ln.lph);
+    if (a.bias) {
+      const bool out = bias == NEG_INF;
+#pragma unroll
+      for (int r = 0; r < RQ; ++r) z[r] = out ? NEG_INF : z[r] + bias;
+      if (__any(out)) {
+#pragma unroll
+        for (int j = 0; j < W; ++j) v[j] = out ? 0.f : v[j];
+      }
+    }
+    bool move = false;
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) move |= z[r] > s[r].m + ATT_SLACK;
+    if (__any(move)) {
+#pragma unroll
+      for (int r = 0; r < RQ; ++r) {
+        const bool up = z[r] > s[r].m + ATT_SLACK;
+        const float f = up ? fast_exp(s[r].m - z[r]) : 1.f;
+        s[r].m = up ? z[r] : s[r].m;
+        s[r].l *= f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) s[r].y[j] *= f;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) {
+      const float p = z[r] == NEG_INF ? 0.f : fast_exp(z[r] - s[r].m);
+      s[r].l += p;
+#pragma unroll
+      for (int j = 0; j < W; ++j) s[r].y[j] = fmaf(p, v[j], s[r].y[j]);
+    }
+  }
+  static __device__ __forceinline__ void join(part& s, const part& o) {
+    const float m = fmaxf(s.m, o.m);
+    const float f = s.m == m ? 1.f : fast_exp(s.m - m), g = o.m == m ? 1.f : fast_exp(o.m - m);  // (both -inf: 1, of nothing)
+    s.m = m;
+    s.l = s.l * f + o.l * g;
+#pragma unroll
+    for (int j = 0; j < W; ++j) s.y[j] = s.y[j] * f + o.y[j] * g;
+  }
+  static __device__ __forceinline__ void store(const att_args& a, const lane_t& ln, int row, const part (&s)[PARTS]) {
+    if (!ln.live) return;
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) {
+      const int h = head(a, ln, r);
+      const float f = s[r].l == 0.f ? 0.f : 1.f / s[r].l;
+      float o[W];
+#pragma unroll
+      for (int j = 0; j < W; ++j) o[j] = s[r].y[j] * f;
+      att_store<T, W, TINY>(static_cast<T*>(a.y) + (int64_t)row * a.ldy + ln.col(h, a.dh), a.dh, o);
+      if (ln.first && a.stats) {
+        float* st = a.stats + ((int64_t)row * a.heads + h) * 2;
+        st[0] = s[r].m;
+        st[1] = s[r].l;
+      }
+    }
+  }
+  // a segment's partial row: heads * dh sums, then (m, l) of each head
+  static __device__ __forceinline__ void store_part(const att_args& a, const lane_t& ln, int seg, const part (&s)[PARTS]) {
+    if (!ln.live) return;
+    float* p = a.part + (int64_t)seg * a.heads * (a.dh + 2);
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) {
+      const int h = head(a, ln, r);
+      att_store<float, W, TINY>(p + ln.col(h, a.dh), a.dh, s[r].y);
+      if (ln.first) {
+        p[a.heads * a.dh + 2 * h] = s[r].m;
+        p[a.heads * a.dh + 2 * h + 1] = s[r].l;
+      }
+    }
+  }
+};
+
+// ---- backward ------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float att_inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }  // (0: the row has nothing)
+// The numbers of a row and head that the columns' pass reads: reference, 1 / l, D.
+__device__ __forceinline__ void att_leave(const att_args& a, int row, int h, float d) {
+  const int64_t at = (int64_t)row * a.heads + h;
+  a.stat[at] = make_float4(a.stats[2 * at], att_inverse(a.stats[2 * at + 1]), d, 0.f);
+}
+__device__ __forceinline__ float4 att_stat(const att_args& a, uint32_t row, int h) {
+  return a.stat[(uint64_t)row * (uint32_t)a.heads + (uint32_t)h];
+}
+// P of a score z whose row has numbers st
+__device__ __forceinline__ float att_weight(float z, const float4& st) { return z == NEG_INF ? 0.f : fast_exp(z - st.x) * st.y; }
+
+// over A's rows: dq, and D
+template <class T_, int W_, int RQ_, bool TINY_>
+struct att_bwd_row {
+  using T = T_;
+  static constexpr int W = W_, RQ = RQ_, RING = RQ == 1 ? 4 : 2, PARTS = RQ;
+  static constexpr bool TINY = TINY_;
+  using lane_t = att_lane<W, TINY>;
+  struct gathered { raw_t<T, W> k, v; };
+  struct requested { raw_t<T, W> q[RQ], dy[RQ]; float2 ml[RQ]; };
+  struct row_t { float q[RQ][W], dy[RQ][W]; float4 st[RQ]; };
+  struct part { float pt[W], p[W], d; };  // of a query head: sums of P t k, P k and P t
+
+  static __device__ __forceinline__ int head(const att_args& a, const lane_t& ln, int r) { return ln.hk * a.group + (int)blockIdx.z * RQ + r; }
+  static __device__ __forceinline__ void clear(part& s) {
+    s.d = 0.f;
+#pragma unroll
+    for (int j = 0; j < W; ++j) s.pt[j] = s.p[j] = 0.f;
+  }
+  static __device__ __forceinline__ void gather(const att_args& a, const lane_t& ln, int col, gathered& o) {
+    const int at = ln.col(ln.hk, a.dh);
+    o.k = att_load<T, W, TINY>(att_row<T>(a.k, col, a.pk) + at, a.dh);
+    o.v = att_load<T, W, TINY>(att_row<T>(a.v, col, a.pv) + at, a.dh);
+  }
+  static __device__ __forceinline__ float2 numbers(const att_args& a, uint32_t row, int h) {
+    return reinterpret_cast<const float2*>(a.stats)[(uint64_t)row * (uint32_t)a.heads + (uint32_t)h];
+  }
+  static __device__ __forceinline__ void request(const att_args& a, const lane_t& ln, int row, bool first, requested& o) {
+    const T *p = att_row<T>(a.q, first ? row : 0, a.pq), *d = att_row<T>(a.dy, first ? row : 0, a.pdy);
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) {
+      const int h = first ? head(a, ln, r) : 0, at = first ? ln.col(h, a.dh) : 0;
+      o.q[r] = att_load<T, W, TINY>(p + at, a.dh);
+      o.dy[r] = att_load<T, W, TINY>(d + at, a.dh);
+      o.ml[r] = numbers(a, first ? row : 0, h);
+    }
+  }
+  static __device__ __forceinline__ void row(const att_args& a, const lane_t& ln, const requested& o, row_t& w) {
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) {
+      att_own<T, W, TINY>(o.q[r], ln, a.scale, w.q[r]);
+      att_own<T, W, TINY>(o.dy[r], ln, 1.f, w.dy[r]);
+      w.st[r] = make_float4(o.ml[r].x, att_inverse(o.ml[r].y), 0.f, 0.f);
+    }
+  }
+  template <int LPG>
+  static __device__ __forceinline__ void edge(const att_args& a, const lane_t& ln, float bias, const gathered& g, const row_t& w, part (&s)[PARTS]) {
+    float k[W], v[W], z[2 * RQ];
+    to_float<T, W>(g.k, k);
+    to_float<T, W>(g.v, v);
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) {
+      z[r] = att_dot<W>(w.q[r], k);
+      z[RQ + r] = att_dot<W>(w.dy[r], v);
+    }
+    att_sums<LPG, 2 * RQ>(z, ln.lph);
+    if (a.bias) {
+      const bool out = bias == NEG_INF;
+#pragma unroll
+      for (int r = 0; r < RQ; ++r) {
+        z[r] = out ? NEG_INF : z[r] + bias;
+        z[RQ + r] = out ? 0.f : z[RQ + r];
+      }
+      if (__any(out)) {
+#pragma unroll
+        for (int j = 0; j < W; ++j) k[j] = out ? 0.f : k[j];
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) {
+      const float p = att_weight(z[r], w.st[r]), pt = p * z[RQ + r];
+      s[r].d += pt;
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        s[r].pt[j] = fmaf(pt, k[j], s[r].pt[j]);
+        s[r].p[j] = fmaf(p, k[j], s[r].p[j]);
+      }
+    }
+  }
+  static __device__ __forceinline__ void join(part& s, const part& o) {
+    s.d += o.d;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      s.pt[j] += o.pt[j];
+      s.p[j] += o.p[j];
+    }
+  }
+  static __device__ __forceinline__ void store(const att_args& a, const lane_t& ln, int row, const part (&s)[PARTS]) {
+    if (!ln.live) return;
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) {
+      const int h = head(a, ln, r);
+      float o[W];
+#pragma unroll
+      for (int j = 0; j < W; ++j) o[j] = (s[r].pt[j] - s[r].d * s[r].p[j]) * a.scale;
+      if (a.y) att_store<T, W, TINY>(static_cast<T*>(a.y) + (int64_t)row * a.ldy + ln.col(h, a.dh), a.dh, o);
+      if (ln.first) att_leave(a, row, h, s[r].d);
+    }
+  }
+  // a segment's partial row: heads * dh sums of P t k, as many of P k, heads of P t
+  static __device__ __forceinline__ void store_part(const att_args& a, const lane_t& ln, int seg, const part (&s)[PARTS]) {
+    if (!ln.live) return;
+    const int width = a.heads * a.dh;
+    float* p = a.part + (int64_t)seg * a.heads * (2 * a.dh + 1);
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) {
+      const int h = head(a, ln, r);
+      att_store<float, W, TINY>(p + ln.col(h, a.dh), a.dh, s[r].pt);
+      att_store<float, W, TINY>(p + width + ln.col(h, a.dh), a.dh, s[r].p);
+      if (ln.first) p[2 * width + h] = s[r].d;
+    }
+  }
+};
+
+// An element of dk / dv: what the passes over other query heads have left (fp32), and the sum of all with the last one's.
+template <class T>
+__device__ __forceinline__ void att_out(const att_args& a, float* carry, T* out, int64_t at_carry, int64_t at, float v) {
+  if (a.pass > 0) v += carry[at_carry];
+  if (a.pass < a.passes - 1) carry[at_carry] = v;
+  else out[at] = (T)v;
+}
+
+// over A^T's rows: dk and dv.  Query heads [pass * RQ, (pass + 1) * RQ) of each key head's; blockIdx.z is not used.
+template <class T_, int W_, int RQ_, bool TINY_>
+struct att_bwd_col {
+  using T = T_;
+  static constexpr int W = W_, RQ = RQ_, RING = RQ == 1 ? 4 : 2, PARTS = 1;
+  static constexpr bool TINY = TINY_;
+  using lane_t = att_lane<W, TINY>;
+  struct gathered { raw_t<T, W> q[RQ], dy[RQ]; float4 st[RQ]; };
+  struct requested { raw_t<T, W> k, v; };
+  struct row_t { float k[W], v[W]; };
+  struct part { float dk[W], dv[W]; };
+
+  static __device__ __forceinline__ void clear(part& s) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) s.dk[j] = s.dv[j] = 0.f;
+  }
+  static __device__ __forceinline__ void gather(const att_args& a, const lane_t& ln, int col, gathered& o) {
+    const T *p = att_row<T>(a.q, col, a.pq), *d = att_row<T>(a.dy, col, a.pdy);
+    const int h0 = ln.hk * a.group + a.pass * RQ;
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) {
+      o.q[r] = att_load<T, W, TINY>(p + ln.col(h0 + r, a.dh), a.dh);
+      o.dy[r] = att_load<T, W, TINY>(d + ln.col(h0 + r, a.dh), a.dh);
+      o.st[r] = att_stat(a, col, h0 + r);
+    }
+  }
+  static __device__ __forceinline__ void request(const att_args& a, const lane_t& ln, int row, bool first, requested& o) {
+    const int at = first ? ln.col(ln.hk, a.dh) : 0;
+    o.k = att_load<T, W, TINY>(att_row<T>(a.k, first ? row : 0, a.pk) + at, a.dh);
+    o.v = att_load<T, W, TINY>(att_row<T>(a.v, first ? row : 0, a.pv) + at, a.dh);
+  }
+  static __device__ __forceinline__ void row(const att_args& a, const lane_t& ln, const requested& o, row_t& w) {
+    att_own<T, W, TINY>(o.k, ln, a.scale, w.k);
+    att_own<T, W, TINY>(o.v, ln, 1.f, w.v);
+  }
+  template <int LPG>
+  static __device__ __forceinline__ void edge(const att_args& a, const lane_t& ln, float bias, const gathered& g, const row_t& w, part (&s)[PARTS]) {
+    float q[RQ][W], dy[RQ][W], z[2 * RQ];
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) {
+      to_float<T, W>(g.q[r], q[r]);
+      to_float<T, W>(g.dy[r], dy[r]);
+      z[r] = att_dot<W>(w.k, q[r]);
+      z[RQ + r] = att_dot<W>(w.v, dy[r]);
+    }
+    att_sums<LPG, 2 * RQ>(z, ln.lph);
+    if (a.bias) {
+      const bool out = bias == NEG_INF;
+#pragma unroll
+      for (int r = 0; r < RQ; ++r) {
+        z[r] = out ? NEG_INF : z[r] + bias;
+        z[RQ + r] = out ? 0.f : z[RQ + r];
+      }
+      if (__any(out)) {
+#pragma unroll
+        for (int r = 0; r < RQ; ++r)
+#pragma unroll
+          for (int j = 0; j < W; ++j) {
+            q[r][j] = out ? 0.f : q[r][j];
+            dy[r][j] = out ? 0.f : dy[r][j];
+          }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) {
+      const float p = att_weight(z[r], g.st[r]), ds = p * (z[RQ + r] - g.st[r].z);
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        s[0].dk[j] = fmaf(ds, q[r][j], s[0].dk[j]);
+        s[0].dv[j] = fmaf(p, dy[r][j], s[0].dv[j]);
+      }
+    }
+  }
+  static __device__ __forceinline__ void join(part& s, const part& o) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      s.dk[j] += o.dk[j];
+      s.dv[j] += o.dv[j];
+    }
+  }
+  static __device__ __forceinline__ void store(const att_args& a, const lane_t& ln, int row, const part (&s)[PARTS]) {
+    if (!ln.live) return;
+    const int at = ln.col(ln.hk, a.dh), width = a.kv_heads * a.dh;
+    float o[2][W];
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      o[0][j] = s[0].dk[j] * a.scale;
+      o[1][j] = s[0].dv[j];
+    }
+    if (a.passes == 1) {
+      att_store<T, W, TINY>(static_cast<T*>(a.y) + (int64_t)row * a.ldy + at, a.dh, o[0]);
+      att_store<T, W, TINY>(static_cast<T*>(a.y2) + (int64_t)row * a.ldy2 + at, a.dh, o[1]);
+    } else {  // (own elements only: a moved-back vector's are the other lane's to add)
+#pragma unroll
+      for (int j = 0; j < W; ++j)
+        if (j >= ln.lo && j < ln.hi) {
+          att_out(a, a.carry, static_cast<T*>(a.y), (int64_t)row * width + at + j, (int64_t)row * a.ldy + at + j, o[0][j]);
+          att_out(a, a.carry2, static_cast<T*>(a.y2), (int64_t)row * width + at + j, (int64_t)row * a.ldy2 + at + j, o[1][j]);
+        }
+    }
+  }
+  // a segment's partial row: dk, then dv
+  static __device__ __forceinline__ void store_part(const att_args& a, const lane_t& ln, int seg, const part (&s)[PARTS]) {
+    if (!ln.live) return;
+    const int width = a.kv_heads * a.dh;
+    float* p = a.part + (int64_t)seg * 2 * width + ln.col(ln.hk, a.dh);
+    float o[W];
+#pragma unroll
+    for (int j = 0; j < W; ++j) o[j] = s[0].dk[j] * a.scale;
+    att_store<float, W, TINY>(p, a.dh, o);
+    att_store<float, W, TINY>(p + width, a.dh, s[0].dv);
+  }
+};
+
+// ---- a pass ----------------------------------------------------------------------------------------------------------
+template <class P, int LPG>
+__global__ void __launch_bounds__(ISP_WG) k_att(isp_view A, const int64_t* __restrict__ indptr, const int32_t* __restrict__ indices,
+                                                const float* __restrict__ bias, att_args a) {
+  __shared__ rn_lds lds;
+  constexpr int G = ISP_WAVE / LPG, RING = P::RING, CHUNK = RING % 4 == 0 ? 2 : 1;
+  using part = typename P::part;
+  constexpr int PARTS = P::PARTS, N = sizeof(part) / sizeof(float);
+  static_assert(ISP_WAVE * sizeof(part) <= sizeof(lds.w[0].ent), "the runs' sums fit the entries' place, a part at a time");
+  const int lane = threadIdx.x & (ISP_WAVE - 1), w = threadIdx.x >> 6;
+  const int item = __builtin_amdgcn_readfirstlane((int)blockIdx.x * ISP_WAVES_PER_WG + w);
+  if (item >= A.n_blocks + A.n_seg) return;
+  const item_range it = locate_item(A, indptr, item);
+  if (it.skip) return;
+  auto& L = lds.w[w];
+  const rn_run R = rn_prepare<G>(it, indptr, indices, bias, nullptr, L, lane);
+  const int g = lane / LPG;
+  const typename P::lane_t ln(a, lane % LPG, LPG / a.lph);
+
+  part st[PARTS], head[PARTS];  // head: the end of a row that began in an earlier run
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) {
+    P::clear(st[k]);
+    P::clear(head[k]);
+  }
+  for (int i = g; i < R.n_empty; i += G) P::store(a, ln, L.dst[RN_EMPTY0 - i], st);
+
+  bool carried = R.mid, ended = false;
+  auto run = [&](auto seg_tag) {
+    constexpr bool SEG = decltype(seg_tag)::value;
+    typename P::gathered x[RING];
+    typename P::requested r[SEG ? 1 : RING];
+    typename P::row_t cur;
+    bool first = true;
+    if constexpr (SEG) {
+      P::request(a, ln, it.src_row, true, r[0]);
+      P::row(a, ln, r[0], cur);
+    }
+    rn_stream<RING, !SEG, !SEG, CHUNK>(
+        L, R,
+        [&](int u, int c, int, int row, bool in_first) {
+          P::gather(a, ln, c, x[u]);
+          if constexpr (!SEG) P::request(a, ln, row, in_first, r[u]);
+        },
+        [&](auto u, float b, int) {
+          if constexpr (!SEG) {
+            if (first) P::row(a, ln, r[u], cur);
+            first = false;
+          }
+          P::template edge<LPG>(a, ln, b, x[u], cur, st);
+        },
+        [&](int, int row) {
+          if (!carried) P::store(a, ln, row, st);
+#pragma unroll
+          for (int k = 0; k < PARTS; ++k) {
+            if (carried) head[k] = st[k];
+            P::clear(st[k]);
+          }
+          carried = false;
+          ended = first = true;
+        });
+  };
+  if (it.is_seg) run(std::true_type{});
+  else run(std::false_type{});
+
+  if (it.is_seg) {  // one row: the groups' parts
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+      const float* v = reinterpret_cast<const float*>(&st[k]);
+#pragma unroll
+      for (int o = LPG; o < ISP_WAVE; o <<= 1) {
+        part other;
+        float* t = reinterpret_cast<float*>(&other);
+#pragma unroll
+        for (int i = 0; i < N; ++i) t[i] = __shfl_xor(v[i], o);
+        P::join(st[k], other);
+      }
+    }
+    if (g == 0) P::store_part(a, ln, it.row, st);
+    return;
+  }
+  if constexpr (G > 1) {  // rows cut by a run boundary: the run in which such a row ends joins the earlier runs' parts
+    const unsigned long long m_end = __ballot(ended), m_mid = __ballot(R.mid);
+    const unsigned long long m_head = m_end & m_mid;
+    if (m_head == 0) return;
+    float* __restrict__ tail = reinterpret_cast<float*>(L.ent);
+    const bool mine = (m_head >> lane) & 1ull;
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+      wave_lds_sync();  // (every entry, or the part before, has been read)
+      const float* v = reinterpret_cast<const float*>(&st[k]);
+#pragma unroll
+      for (int i = 0; i < N; ++i) tail[lane * N + i] = v[i];
+      wave_lds_sync();
+      if (mine) {
+        int j = lane - LPG;
+        for (;;) {
+          part other;
+          float* t = reinterpret_cast<float*>(&other);
+#pragma unroll
+          for (int i = 0; i < N; ++i) t[i] = tail[j * N + i];
+          P::join(head[k], other);
+          if (((m_end >> j) & 1ull) || !((m_mid >> j) & 1ull)) break;  // the row began in that run
+          j -= LPG;
+        }
+      }
+    }
+    if (mine) P::store(a, ln, L.dst[R.k], head);
+  }
+}
+
+// Split rows: their segments' partial rows put together.  A workgroup per row and 64 columns, a wavefront per quarter of the segments,
+// in order; then the quarters, in order.
+template <class T>
+__global__ void __launch_bounds__(ISP_WG) k_att_fwd_fixup(isp_view A, att_args a) {
+  __shared__ float part[ISP_WAVES_PER_WG][3][ISP_WAVE];
+  const int lane = threadIdx.x & (ISP_WAVE - 1), w = threadIdx.x >> 6;
+  const int s0 = A.hub_seg_ptr[blockIdx.x], s1 = A.hub_seg_ptr[blockIdx.x + 1], row = A.hub_rows[blockIdx.x];
+  const int width = a.heads * a.dh, col = (int)blockIdx.y * ISP_WAVE + lane;
+  const int h = col < width ? col / a.dh : 0;
+  const int64_t pitch = (int64_t)a.heads * (a.dh + 2);
+  const int q = (s1 - s0 + ISP_WAVES_PER_WG - 1) / ISP_WAVES_PER_WG;
+  const int lo = s0 + w * q < s1 ? s0 + w * q : s1, hi = lo + q < s1 ? lo + q : s1;
+  float m = NEG_INF, l = 0.f, y = 0.f;
+  if (col < width) {
+#pragma unroll 4
+    for (int s = lo; s < hi; ++s) m = fmaxf(m, a.part[s * pitch + width + 2 * h]);
+#pragma unroll 4
+    for (int s = lo; s < hi; ++s) {
+      const float ms = a.part[s * pitch + width + 2 * h], ls = a.part[s * pitch + width + 2 * h + 1], ys = a.part[s * pitch + col];
+      const float f = ms == m ? 1.f : fast_exp(ms - m);
+      l = fmaf(ls, f, l);
+      y = fmaf(ys, f, y);
+    }
+  }
+  part[w][0][lane] = m;
+  part[w][1][lane] = l;
+  part[w][2][lane] = y;
+  __syncthreads();
+  if (w > 0 || col >= width) return;
+#pragma unroll
+  for (int i = 1; i < ISP_WAVES_PER_WG; ++i) m = fmaxf(m, part[i][0][lane]);
+  l = y = 0.f;
+#pragma unroll
+  for (int i = 0; i < ISP_WAVES_PER_WG; ++i) {
+    const float mi = part[i][0][lane], f = mi == m ? 1.f : fast_exp(mi - m);
+    l = fmaf(part[i][1][lane], f, l);
+    y = fmaf(part[i][2][lane], f, y);
+  }
+  static_cast<T*>(a.y)[(int64_t)row * a.ldy + col] = (T)(l == 0.f ? 0.f : y / l);
+  if (a.stats && col == h * a.dh) {
+    float* st = a.stats + ((int64_t)row * a.heads + h) * 2;
+    st[0] = m;
+    st[1] = l;
+  }
+}
+
+// The sum of column `col` of a split row's partial rows, `pitch` floats each, over the wavefront's quarter of its segments.
+__device__ __forceinline__ float att_quarter(const att_args& a, int lo, int hi, int64_t pitch, int col) {
+  float y = 0.f;
+#pragma unroll 8
+  for (int s = lo; s < hi; ++s) y += a.part[s * pitch + col];
+  return y;
+}
+template <class T>
+__global__ void __launch_bounds__(ISP_WG) k_att_row_fixup(isp_view A, att_args a) {
+  __shared__ float part[ISP_WAVES_PER_WG][3][ISP_WAVE];
+  const int lane = threadIdx.x & (ISP_WAVE - 1), w = threadIdx.x >> 6;
+  const int s0 = A.hub_seg_ptr[blockIdx.x], s1 = A.hub_seg_ptr[blockIdx.x + 1], row = A.hub_rows[blockIdx.x];
+  const int width = a.heads * a.dh, col = (int)blockIdx.y * ISP_WAVE + lane;
+  const int h = col < width ? col / a.dh : 0;
+  const int64_t pitch = (int64_t)a.heads * (2 * a.dh + 1);
+  const int q = (s1 - s0 + ISP_WAVES_PER_WG - 1) / ISP_WAVES_PER_WG;
+  const int lo = s0 + w * q < s1 ? s0 + w * q : s1, hi = lo + q < s1 ? lo + q : s1;
+  if (col < width) {
+    part[w][0][lane] = att_quarter(a, lo, hi, pitch, col);
+    part[w][1][lane] = att_quarter(a, lo, hi, pitch, width + col);
+    part[w][2][lane] = att_quarter(a, lo, hi, pitch, 2 * width + h);
+  }
+  __syncthreads();
+  if (w > 0 || col >= width) return;
+  float t[3];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    t[k] = part[0][k][lane];
+#pragma unroll
+    for (int i = 1; i < ISP_WAVES_PER_WG; ++i) t[k] += part[i][k][lane];
+  }
+  if (a.y) static_cast<T*>(a.y)[(int64_t)row * a.ldy + col] = (T)((t[0] - t[2] * t[1]) * a.scale);
+  if (col == h * a.dh) att_leave(a, row, h, t[2]);
+}
+template <class T>
+__global__ void __launch_bounds__(ISP_WG) k_att_col_fixup(isp_view A, att_args a) {
+  __shared__ float part[ISP_WAVES_PER_WG][ISP_WAVE];
+  const int lane = threadIdx.x & (ISP_WAVE - 1), w = threadIdx.x >> 6;
+  const int s0 = A.hub_seg_ptr[blockIdx.x], s1 = A.hub_seg_ptr[blockIdx.x + 1], row = A.hub_rows[blockIdx.x];
+  const int half = a.kv_heads * a.dh, width = 2 * half, col = (int)blockIdx.y * ISP_WAVE + lane;
+  const int q = (s1 - s0 + ISP_WAVES_PER_WG - 1) / ISP_WAVES_PER_WG;
+  const int lo = s0 + w * q < s1 ? s0 + w * q : s1, hi = lo + q < s1 ? lo + q : s1;
+  float y = col < width ? att_quarter(a, lo, hi, width, col) : 0.f;
+  part[w][lane] = y;
+  __syncthreads();
+  if (w > 0 || col >= width) return;
+#pragma unroll
+  for (int i = 1; i < ISP_WAVES_PER_WG; ++i) y += part[i][lane];
+  if (col < half) att_out(a, a.carry, static_cast<T*>(a.y), (int64_t)row * half + col, (int64_t)row * a.ldy + col, y);
+  else att_out(a, a.carry2, static_cast<T*>(a.y2), (int64_t)row * half + col - half, (int64_t)row * a.ldy2 + col - half, y);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+// chunks: of a key head's query heads, side by side (blockIdx.z)
+template <class P, int LPG>
+isp_status att_launch(const isp_view& v, const att_args& a, int chunks, hipStream_t s) {
+  const int items = v.n_blocks + v.n_seg, hb = LPG / a.lph;
+  if (items == 0) return ISP_OK;
+  const dim3 grid((unsigned)((items + ISP_WAVES_PER_WG - 1) / ISP_WAVES_PER_WG), (unsigned)((a.kv_heads + hb - 1) / hb), (unsigned)chunks);
+  k_att<P, LPG><<<grid, ISP_WG, 0, s>>>(v, v.indptr, v.indices, a.bias ? v.values : nullptr, a);
+  ISP_LAUNCH_CHECK();
+  return ISP_OK;
+}
+// Lanes to a group: as many of the heads as 64 lanes hold.
+template <template <class, int, int, bool> class P, class T, int W, int RQ>
+isp_status att_lanes(const isp_view& v, const att_args& a, int chunks, hipStream_t s) {
+  if (a.dh < W) return att_launch<P<T, W, RQ, true>, 4>(v, a, chunks, s);
+  int lanes = 4;
+  while (lanes < ISP_WAVE && lanes < a.lph * a.kv_heads) lanes *= 2;
+  switch (lanes) {
+    case 4: return att_launch<P<T, W, RQ, false>, 4>(v, a, chunks, s);
+    case 8: return att_launch<P<T, W, RQ, false>, 8>(v, a, chunks, s);
+    case 16: return att_launch<P<T, W, RQ, false>, 16>(v, a, chunks, s);
+    case 32: return att_launch<P<T, W, RQ, false>, 32>(v, a, chunks, s);
+    default: return att_launch<P<T, W, RQ, false>, 64>(v, a, chunks, s);
+  }
+}
+template <template <class, int, int, bool> class P, class T>
+isp_status att_pass(const isp_view& v, const att_args& a, int rq, int chunks, hipStream_t s) {
+  if (rq == 4) return att_lanes<P, T, 4, 4>(v, a, chunks, s);
+  if (rq == 2) return att_lanes<P, T, 4, 2>(v, a, chunks, s);
+  return att_lanes<P, T, 4, 1>(v, a, chunks, s);
+}
+
+template <class T>
+isp_status att_forward(const isp_csr* A, att_args a, hipStream_t s) {
+  const isp_view& v = A->v;
+  const int rq = att_share(a.group);
+  isp_status st = att_pass<att_fwd, T>(v, a, rq, a.group / rq, s);
+  if (st != ISP_OK || v.n_hub == 0) return st;
+  k_att_fwd_fixup<T><<<dim3((unsigned)v.n_hub, (unsigned)((a.heads * a.dh + ISP_WAVE - 1) / ISP_WAVE)), ISP_WG, 0, s>>>(v, a);
+  ISP_LAUNCH_CHECK();
+  return ISP_OK;
+}
+
+template <class T>
+isp_status att_backward(const isp_csr* A, att_args a, const att_grads& o, hipStream_t s) {
+  const isp_view &v = A->v, &vt = A->At ? A->At->v : A->v;
+  const int rq = att_share(a.group), passes = a.group / rq;
+  a.y = o.dq;
+  a.ldy = o.lddq;
+  isp_status st = att_pass<att_bwd_row, T>(v, a, rq, passes, s);
+  if (st != ISP_OK) return st;
+  if (v.n_hub > 0) {
+    k_att_row_fixup<T><<<dim3((unsigned)v.n_hub, (unsigned)((a.heads * a.dh + ISP_WAVE - 1) / ISP_WAVE)), ISP_WG, 0, s>>>(v, a);
+    ISP_LAUNCH_CHECK();
+  }
+  if (!o.dk) return ISP_OK;
+  a.y = o.dk;
+  a.ldy = o.lddk;
+  a.y2 = o.dv;
+  a.ldy2 = o.lddv;
+  a.passes = passes;
+  for (a.pass = 0; a.pass < passes; ++a.pass) {
+    if ((st = att_pass<att_bwd_col, T>(vt, a, rq, 1, s)) != ISP_OK) return st;
+    if (vt.n_hub > 0) {
+      k_att_col_fixup<T><<<dim3((unsigned)vt.n_hub, (unsigned)((2 * a.kv_heads * a.dh + ISP_WAVE - 1) / ISP_WAVE)), ISP_WG, 0, s>>>(vt, a);
+      ISP_LAUNCH_CHECK();
+    }
+  }
+  return ISP_OK;
+}
+
+}  // namespace

@@ -15,6 +15,7 @@
 #include <c10/hip/HIPStream.h>
 #include <hip/hip_runtime_api.h>
 #include <atomic>
+#include <cmath>
 #include <memory>
 #include <mutex>
 #include <vector>
@@ -515,6 +516,87 @@ PyObject* py_label_logprob_backward(PyObject*, PyObject* const* a, Py_ssize_t na
   });
 }
 
+struct Heads {
+  int32_t heads, kv, dim;
+};
+const char* heads_of(const Cell& c, const Mat& Q, const Mat& K, const Mat& V, long heads, long kv, Heads& o) {
+  if (heads <= 0 || kv <= 0 || heads > INT32_MAX || kv > INT32_MAX || Q.d % heads || Q.d == 0) return "Q's rows are `heads` heads of equal width";
+  o.heads = (int32_t)heads;
+  o.kv = (int32_t)kv;
+  o.dim = (int32_t)(Q.d / heads);
+  if (K.d != kv * o.dim || V.d != K.d) return "the rows of K and V are `kv_heads` heads of the width of Q's";
+  if (Q.rows != c.n_rows || K.rows != c.n_cols || V.rows != K.rows) return "Q has A's rows, K and V its columns as rows";
+  if (K.type != Q.type || V.type != Q.type) return "Q, K and V have one type";
+  return nullptr;
+}
+bool same_shape(const Mat& a, const Mat& b) { return a.rows == b.rows && a.d == b.d && a.type == b.type; }
+
+// (cell, Q, K, V, Y, stats, workspace, heads, kv_heads, scale, flags, stream)
+PyObject* py_attention(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  ISP_ARGS(12)
+  Cell* c = cell_of(a[0]);
+  Tensor t[6];
+  for (int i = 1; i < 5; ++i)
+    if (!c || !is_tensor(a[i])) return nullptr;
+  if (!tensors_of(a + 1, t)) return nullptr;
+  const long heads = PyLong_AsLong(a[7]), kv = PyLong_AsLong(a[8]);
+  const double scale = PyFloat_AsDouble(a[9]);
+  const unsigned flags = (unsigned)PyLong_AsUnsignedLong(a[10]);
+  const Where w = stream_of(a[11]);
+  if (PyErr_Occurred()) return nullptr;
+  Mat Q, K, V, Y;
+  Heads H;
+  void *stats, *ws;
+  size_t bytes;
+  ISP_REFUSE(mat_of(t[0], Q));
+  ISP_REFUSE(mat_of(t[1], K));
+  ISP_REFUSE(mat_of(t[2], V));
+  ISP_REFUSE(mat_of(t[3], Y));
+  ISP_REFUSE(heads_of(*c, Q, K, V, heads, kv, H));
+  ISP_REFUSE_IF(!same_shape(Q, Y), "Q and Y have one shape and type");
+  ISP_REFUSE(array_of(t[4], at::kFloat, 2 * Q.rows * heads, &stats));
+  ISP_REFUSE(bytes_of(t[5], &ws, &bytes));
+  return call(c, w, [&](isp_csr_t* h, void* s) {
+    return isp_attention(h, Q.p, Q.ld, K.p, K.ld, V.p, V.ld, H.heads, H.kv, H.dim, (float)scale, flags, Q.type, Y.p, Y.ld, (float*)stats, ws, bytes, s);
+  });
+}
+
+// (cell, Q, K, V, stats, dY, dQ, dK, dV, workspace, heads, kv_heads, scale, flags, stream)
+PyObject* py_attention_backward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  ISP_ARGS(15)
+  Cell* c = cell_of(a[0]);
+  Tensor t[9];
+  for (int i = 1; i < 6; ++i)
+    if (!c || !is_tensor(a[i])) return nullptr;
+  if (!tensors_of(a + 1, t)) return nullptr;
+  const long heads = PyLong_AsLong(a[10]), kv = PyLong_AsLong(a[11]);
+  const double scale = PyFloat_AsDouble(a[12]);
+  const unsigned flags = (unsigned)PyLong_AsUnsignedLong(a[13]);
+  const Where w = stream_of(a[14]);
+  if (PyErr_Occurred()) return nullptr;
+  Mat Q, K, V, G, O[3] = {};
+  Heads H;
+  void *stats, *ws;
+  size_t bytes;
+  ISP_REFUSE(mat_of(t[0], Q));
+  ISP_REFUSE(mat_of(t[1], K));
+  ISP_REFUSE(mat_of(t[2], V));
+  ISP_REFUSE(mat_of(t[4], G));
+  ISP_REFUSE(heads_of(*c, Q, K, V, heads, kv, H));
+  ISP_REFUSE_IF(!same_shape(Q, G), "Q and dY have one shape and type");
+  for (int i = 0; i < 3; ++i)
+    if (t[5 + i].defined()) {
+      ISP_REFUSE(mat_of(t[5 + i], O[i]));
+      ISP_REFUSE_IF(!same_shape(O[i], i == 0 ? Q : K), "a gradient has its operand's shape and type");
+    }
+  ISP_REFUSE(array_of(t[3], at::kFloat, 2 * Q.rows * heads, &stats));
+  ISP_REFUSE(bytes_of(t[8], &ws, &bytes));
+  return call(c, w, [&](isp_csr_t* h, void* s) {
+    return isp_attention_backward(h, Q.p, Q.ld, K.p, K.ld, V.p, V.ld, H.heads, H.kv, H.dim, (float)scale, flags, Q.type, (const float*)stats, G.p, G.ld,
+                                  O[0].p, O[0].ld, O[1].p, O[1].ld, O[2].p, O[2].ld, ws, bytes, s);
+  });
+}
+
 // ---- autograd -------------------------------------------------------------------------------------------------
 // The same operations as nodes of torch's graph.  The backward touches the interpreter only when a transpose has to
 // be built or a call fails.  (4,096 rows, 32 columns, forward + backward: 112 -> 44 us of host time; a multiplication by
@@ -985,6 +1067,108 @@ PyObject* py_ag_label_logprob(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+struct AttentionBackward : torch::autograd::Node {
+  GraphPtr graph;
+  SavedVariable Q, K, V;
+  Tensor stats;
+  Heads H{};
+  float scale = 0.f;
+  unsigned flags = 0;
+  std::string name() const override { return "IspAttentionBackward"; }
+  void release_variables() override {
+    for (SavedVariable* v : {&Q, &K, &V}) v->reset_data();
+    stats.reset();
+  }
+  variable_list apply(variable_list&& grads) override {
+    variable_list out(3);
+    if (!grads[0].defined()) return out;
+    at::NoGradGuard no_grad;
+    const Tensor q = Q.unpack(), k = K.unpack(), v = V.unpack(), dY = rows_of(grads[0]);
+    const bool rows = task_should_compute_output(0), cols = task_should_compute_output(1) || task_should_compute_output(2);
+    if (cols) transpose(*graph);
+    else sync_values(*graph);
+    const Mat MQ = mat(q), MK = mat(k), MV = mat(v), G = mat(dY);
+    Mat O[3] = {};
+    if (rows) {
+      out[0] = at::empty({MQ.rows, MQ.d}, q.options().requires_grad(false));
+      O[0] = mat(out[0]);
+    }
+    if (cols)
+      for (int i = 1; i < 3; ++i) {
+        out[i] = at::empty({MK.rows, MK.d}, k.options().requires_grad(false));
+        O[i] = mat(out[i]);
+      }
+    size_t bytes = 0;
+    check(isp_attention_backward_workspace(graph->A->h.load(), H.heads, H.kv, H.dim, &bytes));
+    const Tensor ws = workspace_like(q, bytes);
+    run(*graph->A, [&](isp_csr_t* h, void* s) {
+      return isp_attention_backward(h, MQ.p, MQ.ld, MK.p, MK.ld, MV.p, MV.ld, H.heads, H.kv, H.dim, scale, flags, MQ.type, stats.data_ptr<float>(),
+                                    G.p, G.ld, O[0].p, O[0].ld, O[1].p, O[1].ld, O[2].p, O[2].ld, ws.data_ptr(), bytes, s);
+    });
+    return out;
+  }
+};
+
+// (graph, Q, K, V, heads, kv_heads, scale or None, flags) -> Y
+PyObject* py_ag_attention(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  ISP_ARGS(8)
+  GraphPtr g = graph_of(a[0]);
+  for (int i = 1; i < 4; ++i)
+    if (!is_tensor(a[i])) return nullptr;
+  Tensor t[3];
+  if (!tensors_of(a + 1, t)) return nullptr;
+  const long heads = PyLong_AsLong(a[4]), kv = PyLong_AsLong(a[5]);
+  double scale = a[6] == Py_None ? 0. : PyFloat_AsDouble(a[6]);
+  const unsigned flags = (unsigned)PyLong_AsUnsignedLong(a[7]);
+  if (PyErr_Occurred()) return nullptr;
+  for (const Tensor& v : t)
+    if (!no_tangent(v)) return nullptr;
+  Tensor Y;
+  {
+    pybind11::gil_scoped_release release;
+    const bool grad = torch::autograd::compute_requires_grad(t[0], t[1], t[2]);
+    Tensor q, k, v, stats;
+    Heads H;
+    {
+      at::NoGradGuard no_grad;
+      q = rows_of(t[0]);
+      k = rows_of(t[1]);
+      v = rows_of(t[2]);
+      const Mat MQ = mat(q), MK = mat(k), MV = mat(v);
+      if (const char* bad = heads_of(*g->A, MQ, MK, MV, heads, kv, H)) assertion(bad);
+      if (a[6] == Py_None) scale = 1. / std::sqrt((double)H.dim);
+      Y = at::empty({MQ.rows, MQ.d}, q.options().requires_grad(false));
+      const Mat O = mat(Y);
+      if (grad) stats = floats_like(q, {MQ.rows, heads, 2});
+      size_t bytes = 0;
+      check(isp_attention_workspace(g->A->h.load(), H.heads, H.dim, &bytes));
+      Tensor ws;
+      if (bytes) ws = workspace_like(q, bytes);
+      sync_values(*g);
+      run(*g->A, [&](isp_csr_t* h, void* s) {
+        return isp_attention(h, MQ.p, MQ.ld, MK.p, MK.ld, MV.p, MV.ld, H.heads, H.kv, H.dim, (float)scale, flags, MQ.type, O.p, O.ld,
+                             grad ? stats.data_ptr<float>() : nullptr, bytes ? ws.data_ptr() : nullptr, bytes, s);
+      });
+    }
+    if (grad) {
+      auto node = std::shared_ptr<AttentionBackward>(new AttentionBackward(), torch::autograd::deleteNode);
+      node->set_next_edges(torch::autograd::collect_next_edges(t[0], t[1], t[2]));
+      node->graph = g;
+      node->Q = SavedVariable(q, false);
+      node->K = SavedVariable(k, false);
+      node->V = SavedVariable(v, false);
+      node->stats = stats;
+      node->H = H;
+      node->scale = (float)scale;
+      node->flags = flags;
+      torch::autograd::set_history(Y, node);
+    }
+  }
+  return THPVariable_Wrap(Y);
+  END_HANDLE_TH_ERRORS
+}
+
 // (binding._check, binding.csr_transpose_cached)
 PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   ISP_ARGS(2)
@@ -1027,6 +1211,9 @@ PyMethodDef methods[] = {
     ISP_DEF("label_logprob_backward", py_label_logprob_backward),
     ISP_DEF("ag_layer_norm", py_ag_layer_norm),
     ISP_DEF("ag_label_logprob", py_ag_label_logprob),
+    ISP_DEF("attention", py_attention),
+    ISP_DEF("attention_backward", py_attention_backward),
+    ISP_DEF("ag_attention", py_ag_attention),
     ISP_DEF("graph", py_graph),
     ISP_DEF("graph_sync", py_graph_sync),
     ISP_DEF("ag_spmm", py_ag_spmm),

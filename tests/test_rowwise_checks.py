@@ -1,4 +1,4 @@
-"""What the row-wise operators refuse, on the CPU: arguments are looked at before any device work."""
+"""What the row-wise operators and the attention refuse, on the CPU: arguments are looked at before any device work."""
 import ctypes
 
 import numpy as np
@@ -58,7 +58,19 @@ def test_label_logprob_at_the_c_boundary(lib):
         assert g(**bad) == EINVAL, bad
 
 
+def test_attention_at_the_c_boundary(lib):
+    need = ctypes.c_size_t()
+    assert lib.isp_attention_workspace(None, 2, 8, ctypes.byref(need)) == EINVAL and lib.isp_attention_workspace(None, 2, 8, None) == EINVAL
+    assert lib.isp_attention_backward_workspace(None, 2, 2, 8, ctypes.byref(need)) == EINVAL
+    assert lib.isp_attention(None, P, 16, P, 16, P, 16, 2, 2, 8, 1.0, 0, 0, P, 16, None, None, 0, None) == EINVAL
+    assert lib.isp_attention_backward(None, P, 16, P, 16, P, 16, 2, 2, 8, 1.0, 0, 0, P, P, 16, P, 16, P, 16, P, 16, None, 0, None) == EINVAL
+
+
 NOT_TENSORS = [np.zeros((4, 8), np.float32), [[1.0, 2.0]], "x", 3.0]
+
+
+def cell(nat):
+    return nat.cell(0, 4, 4, 6)  # a NULL handle of a 4 x 4 matrix
 
 
 @pytest.mark.parametrize("x", NOT_TENSORS, ids=lambda x: type(x).__name__)
@@ -68,7 +80,10 @@ def test_operands_must_be_tensors(x):
                  lambda: nat.layer_norm(t, t, x, None, None, None, 1e-5, 0), lambda: nat.layer_norm_backward(t, x, t, t, t, None, None, None, None, 0),
                  lambda: nat.label_logprob(x, t, t, None, None, None, None, None, 0), lambda: nat.label_logprob(t, x, t, None, None, None, None, None, 0),
                  lambda: nat.label_logprob_backward(x, t, t, t, t, t, t, 0), lambda: ag.layer_norm(x), lambda: ag.layer_norm(t, x),
-                 lambda: ag.label_logprob(x, t), lambda: ag.label_logprob(t, x)):
+                 lambda: ag.label_logprob(x, t), lambda: ag.label_logprob(t, x), lambda: nat.attention(cell(nat), x, t, t, t, None, None, 1, 1, 1.0, 0, 0),
+                 lambda: nat.attention(cell(nat), t, t, t, x, None, None, 1, 1, 1.0, 0, 0), lambda: nat.attention(cell(nat), t, t, t, t, x, None, 1, 1, 1.0, 0, 0),
+                 lambda: nat.attention_backward(cell(nat), t, t, t, x, t, None, None, None, None, 1, 1, 1.0, 0, 0),
+                 lambda: nat.ag_attention(nat.graph(cell(nat), object(), None), t, x, t, 1, 1, None, 0)):
         with pytest.raises(TypeError):
             call()
 
@@ -76,7 +91,9 @@ def test_operands_must_be_tensors(x):
 def test_cpu_tensors_are_refused():
     t, y = torch.zeros(4, 8), torch.zeros(4, dtype=torch.int64)
     for call in (lambda: isp.layer_norm(t, t), lambda: isp.layer_norm_backward(t, t, t, t[:, 0], t[:, 0], workspace=t), lambda: ag.layer_norm(t),
-                 lambda: isp.label_logprob(t, y, t[:, 0]), lambda: isp.label_logprob_backward(t, y, t, t[:, 0], t), lambda: ag.label_logprob(t, y)):
+                 lambda: isp.label_logprob(t, y, t[:, 0]), lambda: isp.label_logprob_backward(t, y, t, t[:, 0], t), lambda: ag.label_logprob(t, y),
+                 lambda: binding._native().attention(cell(binding._native()), t, t, t, t, None, None, 1, 1, 1.0, 0, 0),
+                 lambda: binding._native().ag_attention(binding._native().graph(cell(binding._native()), object(), None), t, t, t, 1, 1, None, 0)):
         with pytest.raises(AssertionError):
             call()
 
@@ -87,7 +104,8 @@ def test_forward_mode_is_refused():
     with fw.dual_level():
         x = fw.make_dual(t, torch.ones(4, 8))
         w = fw.make_dual(t[0], torch.ones(8))
-        for call in (lambda: ag.layer_norm(x), lambda: ag.layer_norm(t, w), lambda: ag.layer_norm(t, None, w), lambda: ag.label_logprob(x, y)):
+        for call in (lambda: ag.layer_norm(x), lambda: ag.layer_norm(t, w), lambda: ag.layer_norm(t, None, w), lambda: ag.label_logprob(x, y),
+                     lambda: binding._native().ag_attention(binding._native().graph(cell(binding._native()), object(), None), t, x, t, 1, 1, None, 0)):
             with pytest.raises(NotImplementedError):
                 call()
 
