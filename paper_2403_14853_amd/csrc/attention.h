@@ -26,6 +26,8 @@ namespace {
 using namespace isp_dev;
 
 constexpr float ATT_SLACK = 8.f;
+// The reference of a row that has met nothing: finite, so that differences to it are numbers; a score of -inf is below it, too.
+constexpr float ATT_NONE = -3.402823466e38f;
 
 // Where a lane works.
 template <int W, bool TINY>
@@ -111,31 +113,34 @@ __device__ __forceinline__ const T* att_row(const void* base, uint32_t row, uint
 template <class T_, int W_, int RQ_, bool TINY_>
 struct att_fwd {
   using T = T_;
-  static constexpr int W = W_, RQ = RQ_, RING = RQ == 1 ? 4 : 2, PARTS = RQ;
+  static constexpr int W = W_, RQ = RQ_, RING = 4, PARTS = RQ;
   static constexpr bool TINY = TINY_;
   using lane_t = att_lane<W, TINY>;
   struct gathered { raw_t<T, W> k, v; };
+  struct source { const T *k, *v; };  // the lane's columns of row 0
   struct requested { raw_t<T, W> q[RQ]; };
   struct row_t { float q[RQ][W]; };
   struct part { float y[W], m, l; };  // of a query head
 
   static __device__ __forceinline__ int head(const att_args& a, const lane_t& ln, int r) { return ln.hk * a.group + (int)blockIdx.z * RQ + r; }
   static __device__ __forceinline__ void clear(part& s) {
-    s.m = NEG_INF;
+    s.m = ATT_NONE;
     s.l = 0.f;
 #pragma unroll
     for (int j = 0; j < W; ++j) s.y[j] = 0.f;
   }
-  static __device__ __forceinline__ void gather(const att_args& a, const lane_t& ln, int col, gathered& o) {
+  static __device__ __forceinline__ source sources(const att_args& a, const lane_t& ln) {
     const int at = ln.col(ln.hk, a.dh);
-    o.k = att_load<T, W, TINY>(att_row<T>(a.k, col, a.pk) + at, a.dh);
-    o.v = att_load<T, W, TINY>(att_row<T>(a.v, col, a.pv) + at, a.dh);
+    return {static_cast<const T*>(a.k) + at, static_cast<const T*>(a.v) + at};
   }
-  // (other steps than a row's first read one and the same line, which keeps the number of loads per step fixed)
-  static __device__ __forceinline__ void request(const att_args& a, const lane_t& ln, int row, bool first, requested& o) {
-    const T* p = att_row<T>(a.q, first ? row : 0, a.pq);
+  static __device__ __forceinline__ void gather(const att_args& a, const source& o, int col, gathered& x) {
+    x.k = att_load<T, W, TINY>(att_row<T>(o.k, col, a.pk), a.dh);
+    x.v = att_load<T, W, TINY>(att_row<T>(o.v, col, a.pv), a.dh);
+  }
+  static __device__ __forceinline__ void request(const att_args& a, const lane_t& ln, int row, requested& o) {
+    const T* p = att_row<T>(a.q, row, a.pq) + ln.col(head(a, ln, 0), a.dh);
 #pragma unroll
-    for (int r = 0; r < RQ; ++r) o.q[r] = att_load<T, W, TINY>(p + (first ? ln.col(head(a, ln, r), a.dh) : 0), a.dh);
+    for (int r = 0; r < RQ; ++r) o.q[r] = att_load<T, W, TINY>(p + r * a.dh, a.dh);
   }
   static __device__ __forceinline__ void row(const att_args& a, const lane_t& ln, const requested& o, row_t& w) {
 #pragma unroll
@@ -158,15 +163,20 @@ struct att_fwd {
         for (int j = 0; j < W; ++j) v[j] = out ? 0.f : v[j];
       }
     }
+    float gap[RQ];
     bool move = false;
 #pragma unroll
-    for (int r = 0; r < RQ; ++r) move |= z[r] > s[r].m + ATT_SLACK;
+    for (int r = 0; r < RQ; ++r) {
+      gap[r] = z[r] - s[r].m;
+      move |= gap[r] > ATT_SLACK;
+    }
     if (__any(move)) {
 #pragma unroll
       for (int r = 0; r < RQ; ++r) {
-        const bool up = z[r] > s[r].m + ATT_SLACK;
-        const float f = up ? fast_exp(s[r].m - z[r]) : 1.f;
+        const bool up = gap[r] > ATT_SLACK;
+        const float f = up ? fast_exp(-gap[r]) : 1.f;
         s[r].m = up ? z[r] : s[r].m;
+        gap[r] = up ? z[r] - z[r] : gap[r];  // (0; +inf: NaN)
         s[r].l *= f;
 #pragma unroll
         for (int j = 0; j < W; ++j) s[r].y[j] *= f;
@@ -174,7 +184,7 @@ struct att_fwd {
     }
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
-      const float p = z[r] == NEG_INF ? 0.f : fast_exp(z[r] - s[r].m);
+      const float p = fast_exp(gap[r]);
       s[r].l += p;
 #pragma unroll
       for (int j = 0; j < W; ++j) s[r].y[j] = fmaf(p, v[j], s[r].y[j]);
@@ -182,7 +192,7 @@ struct att_fwd {
   }
   static __device__ __forceinline__ void join(part& s, const part& o) {
     const float m = fmaxf(s.m, o.m);
-    const float f = s.m == m ? 1.f : fast_exp(s.m - m), g = o.m == m ? 1.f : fast_exp(o.m - m);  // (both -inf: 1, of nothing)
+    const float f = s.m == m ? 1.f : fast_exp(s.m - m), g = o.m == m ? 1.f : fast_exp(o.m - m);  // (both none: 1, of nothing)
     s.m = m;
     s.l = s.l * f + o.l * g;
 #pragma unroll
@@ -228,20 +238,18 @@ __device__ __forceinline__ void att_leave(const att_args& a, int row, int h, flo
   const int64_t at = (int64_t)row * a.heads + h;
   a.stat[at] = make_float4(a.stats[2 * at], att_inverse(a.stats[2 * at + 1]), d, 0.f);
 }
-__device__ __forceinline__ float4 att_stat(const att_args& a, uint32_t row, int h) {
-  return a.stat[(uint64_t)row * (uint32_t)a.heads + (uint32_t)h];
-}
 // P of a score z whose row has numbers st
-__device__ __forceinline__ float att_weight(float z, const float4& st) { return z == NEG_INF ? 0.f : fast_exp(z - st.x) * st.y; }
+__device__ __forceinline__ float att_weight(float z, const float4& st) { return fast_exp(z - st.x) * st.y; }
 
 // over A's rows: dq, and D
 template <class T_, int W_, int RQ_, bool TINY_>
 struct att_bwd_row {
   using T = T_;
-  static constexpr int W = W_, RQ = RQ_, RING = RQ == 1 ? 4 : 2, PARTS = RQ;
+  static constexpr int W = W_, RQ = RQ_, RING = 4, PARTS = RQ;
   static constexpr bool TINY = TINY_;
   using lane_t = att_lane<W, TINY>;
   struct gathered { raw_t<T, W> k, v; };
+  struct source { const T *k, *v; };
   struct requested { raw_t<T, W> q[RQ], dy[RQ]; float2 ml[RQ]; };
   struct row_t { float q[RQ][W], dy[RQ][W]; float4 st[RQ]; };
   struct part { float pt[W], p[W], d; };  // of a query head: sums of P t k, P k and P t
@@ -252,22 +260,23 @@ struct att_bwd_row {
 #pragma unroll
     for (int j = 0; j < W; ++j) s.pt[j] = s.p[j] = 0.f;
   }
-  static __device__ __forceinline__ void gather(const att_args& a, const lane_t& ln, int col, gathered& o) {
+  static __device__ __forceinline__ source sources(const att_args& a, const lane_t& ln) {
     const int at = ln.col(ln.hk, a.dh);
-    o.k = att_load<T, W, TINY>(att_row<T>(a.k, col, a.pk) + at, a.dh);
-    o.v = att_load<T, W, TINY>(att_row<T>(a.v, col, a.pv) + at, a.dh);
+    return {static_cast<const T*>(a.k) + at, static_cast<const T*>(a.v) + at};
   }
-  static __device__ __forceinline__ float2 numbers(const att_args& a, uint32_t row, int h) {
-    return reinterpret_cast<const float2*>(a.stats)[(uint64_t)row * (uint32_t)a.heads + (uint32_t)h];
+  static __device__ __forceinline__ void gather(const att_args& a, const source& o, int col, gathered& x) {
+    x.k = att_load<T, W, TINY>(att_row<T>(o.k, col, a.pk), a.dh);
+    x.v = att_load<T, W, TINY>(att_row<T>(o.v, col, a.pv), a.dh);
   }
-  static __device__ __forceinline__ void request(const att_args& a, const lane_t& ln, int row, bool first, requested& o) {
-    const T *p = att_row<T>(a.q, first ? row : 0, a.pq), *d = att_row<T>(a.dy, first ? row : 0, a.pdy);
+  static __device__ __forceinline__ void request(const att_args& a, const lane_t& ln, int row, requested& o) {
+    const int h = head(a, ln, 0), at = ln.col(h, a.dh);
+    const T *p = att_row<T>(a.q, row, a.pq) + at, *d = att_row<T>(a.dy, row, a.pdy) + at;
+    const float2* ml = reinterpret_cast<const float2*>(a.stats) + ((uint64_t)(uint32_t)row * (uint32_t)a.heads + (uint32_t)h);
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
-      const int h = first ? head(a, ln, r) : 0, at = first ? ln.col(h, a.dh) : 0;
-      o.q[r] = att_load<T, W, TINY>(p + at, a.dh);
-      o.dy[r] = att_load<T, W, TINY>(d + at, a.dh);
-      o.ml[r] = numbers(a, first ? row : 0, h);
+      o.q[r] = att_load<T, W, TINY>(p + r * a.dh, a.dh);
+      o.dy[r] = att_load<T, W, TINY>(d + r * a.dh, a.dh);
+      o.ml[r] = ml[r];
     }
   }
   static __device__ __forceinline__ void row(const att_args& a, const lane_t& ln, const requested& o, row_t& w) {
@@ -363,6 +372,7 @@ struct att_bwd_col {
   static constexpr bool TINY = TINY_;
   using lane_t = att_lane<W, TINY>;
   struct gathered { raw_t<T, W> q[RQ], dy[RQ]; float4 st[RQ]; };
+  struct source { const T *q, *dy; const float4* st; };
   struct requested { raw_t<T, W> k, v; };
   struct row_t { float k[W], v[W]; };
   struct part { float dk[W], dv[W]; };
@@ -371,20 +381,24 @@ struct att_bwd_col {
 #pragma unroll
     for (int j = 0; j < W; ++j) s.dk[j] = s.dv[j] = 0.f;
   }
-  static __device__ __forceinline__ void gather(const att_args& a, const lane_t& ln, int col, gathered& o) {
-    const T *p = att_row<T>(a.q, col, a.pq), *d = att_row<T>(a.dy, col, a.pdy);
-    const int h0 = ln.hk * a.group + a.pass * RQ;
+  static __device__ __forceinline__ source sources(const att_args& a, const lane_t& ln) {
+    const int h0 = ln.hk * a.group + a.pass * RQ, at = ln.col(h0, a.dh);
+    return {static_cast<const T*>(a.q) + at, static_cast<const T*>(a.dy) + at, a.stat + h0};
+  }
+  static __device__ __forceinline__ void gather(const att_args& a, const source& o, int col, gathered& x) {
+    const T *p = att_row<T>(o.q, col, a.pq), *d = att_row<T>(o.dy, col, a.pdy);
+    const float4* st = att_row<float4>(o.st, col, (uint32_t)a.heads * (uint32_t)sizeof(float4));
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
-      o.q[r] = att_load<T, W, TINY>(p + ln.col(h0 + r, a.dh), a.dh);
-      o.dy[r] = att_load<T, W, TINY>(d + ln.col(h0 + r, a.dh), a.dh);
-      o.st[r] = att_stat(a, col, h0 + r);
+      x.q[r] = att_load<T, W, TINY>(p + r * a.dh, a.dh);
+      x.dy[r] = att_load<T, W, TINY>(d + r * a.dh, a.dh);
+      x.st[r] = st[r];
     }
   }
-  static __device__ __forceinline__ void request(const att_args& a, const lane_t& ln, int row, bool first, requested& o) {
-    const int at = first ? ln.col(ln.hk, a.dh) : 0;
-    o.k = att_load<T, W, TINY>(att_row<T>(a.k, first ? row : 0, a.pk) + at, a.dh);
-    o.v = att_load<T, W, TINY>(att_row<T>(a.v, first ? row : 0, a.pv) + at, a.dh);
+  static __device__ __forceinline__ void request(const att_args& a, const lane_t& ln, int row, requested& o) {
+    const int at = ln.col(ln.hk, a.dh);
+    o.k = att_load<T, W, TINY>(att_row<T>(a.k, row, a.pk) + at, a.dh);
+    o.v = att_load<T, W, TINY>(att_row<T>(a.v, row, a.pv) + at, a.dh);
   }
   static __device__ __forceinline__ void row(const att_args& a, const lane_t& ln, const requested& o, row_t& w) {
     att_own<T, W, TINY>(o.k, ln, a.scale, w.k);
@@ -496,39 +510,32 @@ __global__ void __launch_bounds__(ISP_WG) k_att(isp_view A, const int64_t* __res
   }
   for (int i = g; i < R.n_empty; i += G) P::store(a, ln, L.dst[RN_EMPTY0 - i], st);
 
+  if (R.steps == 0) return;  // (no entries: the operands may not be there)
+
   bool carried = R.mid, ended = false;
+  const typename P::source src = P::sources(a, ln);
   auto run = [&](auto seg_tag) {
     constexpr bool SEG = decltype(seg_tag)::value;
     typename P::gathered x[RING];
-    typename P::requested r[SEG ? 1 : RING];
+    typename P::requested next;  // the row after the one at work, requested when that one began
     typename P::row_t cur;
-    bool first = true;
-    if constexpr (SEG) {
-      P::request(a, ln, it.src_row, true, r[0]);
-      P::row(a, ln, r[0], cur);
-    }
-    rn_stream<RING, !SEG, !SEG, CHUNK>(
-        L, R,
-        [&](int u, int c, int, int row, bool in_first) {
-          P::gather(a, ln, c, x[u]);
-          if constexpr (!SEG) P::request(a, ln, row, in_first, r[u]);
-        },
-        [&](auto u, float b, int) {
-          if constexpr (!SEG) {
-            if (first) P::row(a, ln, r[u], cur);
-            first = false;
-          }
-          P::template edge<LPG>(a, ln, b, x[u], cur, st);
-        },
-        [&](int, int row) {
+    P::request(a, ln, SEG ? it.src_row : L.dst[R.k], next);
+    P::row(a, ln, next, cur);
+    if constexpr (!SEG) P::request(a, ln, L.dst[R.k + 1], next);
+    rn_stream<RING, !SEG, false, CHUNK>(
+        L, R, [&](int u, int c, int, int, bool) { P::gather(a, src, c, x[u]); },
+        [&](auto u, float b, int) { P::template edge<LPG>(a, ln, b, x[u], cur, st); },
+        [&](int k, int row) {
           if (!carried) P::store(a, ln, row, st);
 #pragma unroll
-          for (int k = 0; k < PARTS; ++k) {
-            if (carried) head[k] = st[k];
-            P::clear(st[k]);
+          for (int i = 0; i < PARTS; ++i) {
+            if (carried) head[i] = st[i];
+            P::clear(st[i]);
           }
           carried = false;
-          ended = first = true;
+          ended = true;
+          P::row(a, ln, next, cur);
+          P::request(a, ln, L.dst[k + 2], next);
         });
   };
   if (it.is_seg) run(std::true_type{});
@@ -592,7 +599,7 @@ __global__ void __launch_bounds__(ISP_WG) k_att_fwd_fixup(isp_view A, att_args a
   const int64_t pitch = (int64_t)a.heads * (a.dh + 2);
   const int q = (s1 - s0 + ISP_WAVES_PER_WG - 1) / ISP_WAVES_PER_WG;
   const int lo = s0 + w * q < s1 ? s0 + w * q : s1, hi = lo + q < s1 ? lo + q : s1;
-  float m = NEG_INF, l = 0.f, y = 0.f;
+  float m = ATT_NONE, l = 0.f, y = 0.f;
   if (col < width) {
 #pragma unroll 4
     for (int s = lo; s < hi; ++s) m = fmaxf(m, a.part[s * pitch + width + 2 * h]);
