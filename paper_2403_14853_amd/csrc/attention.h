@@ -36,6 +36,7 @@ struct att_lane {
   int hk;     // key head (of a lane without one: the last)
   int c;      // first column of its vector within the head: the last vector of a head moves back to end with it
   int lo, hi; // elements [lo, hi) of the vector are its own (a moved-back vector's leading ones belong to the vector before)
+  float own[W], scaled[W];  // 1 or the scale for those, else 0
   bool live, first;  // first: has the head's first column
   __device__ __forceinline__ att_lane(const att_args& a, int q, int hb) {
     lph = a.lph;
@@ -46,6 +47,11 @@ struct att_lane {
     lo = live ? c0 - c : W;
     hi = TINY ? a.dh : W;
     first = live && c0 == 0;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      own[j] = j >= lo && j < hi ? 1.f : 0.f;
+      scaled[j] = j >= lo && j < hi ? a.scale : 0.f;
+    }
   }
   __device__ __forceinline__ int col(int head, int dh) const { return head * dh + c; }
 };
@@ -96,13 +102,17 @@ __device__ __forceinline__ float att_dot(const float (&a)[W], const float (&b)[W
   for (int j = 1; j < W; ++j) s = fmaf(a[j], b[j], s);
   return s;
 }
-// A lane's elements of a row operand, times f; those that are not its own as zero, so that they add nothing to a dot product.
-template <class T, int W, bool TINY>
-__device__ __forceinline__ void att_own(const raw_t<T, W>& r, const att_lane<W, TINY>& ln, float f, float (&o)[W]) {
+// A lane's elements of a row operand times f, lane.own or lane.scaled: those that are not its own count for nothing in a dot product.  (They are of
+// the same head, or the head is nobody's: an infinity or NaN among them is in the dot product anyway.)
+template <class T, int W>
+__device__ __forceinline__ void att_own(const raw_t<T, W>& r, const float (&f)[W], float (&o)[W]) {
   to_float<T, W>(r, o);
 #pragma unroll
-  for (int j = 0; j < W; ++j) o[j] = j >= ln.lo && j < ln.hi ? o[j] * f : 0.f;
+  for (int j = 0; j < W; ++j) o[j] *= f[j];
 }
+
+// 1 / l by the hardware's reciprocal (about 1 ulp); 0 where the row has nothing.
+__device__ __forceinline__ float att_inverse(float l) { return l == 0.f ? 0.f : __builtin_amdgcn_rcpf(l); }
 
 template <class T>
 __device__ __forceinline__ const T* att_row(const void* base, uint32_t row, uint32_t pitch) {  // (pitch in bytes)
@@ -113,7 +123,8 @@ __device__ __forceinline__ const T* att_row(const void* base, uint32_t row, uint
 template <class T_, int W_, int RQ_, bool TINY_>
 struct att_fwd {
   using T = T_;
-  static constexpr int W = W_, RQ = RQ_, RING = 4, PARTS = RQ;
+  static constexpr int W = W_, RQ = RQ_, RING = 4, PARTS = RQ, MOST = 4, WAVES = 1;
+  static constexpr bool WIDE = true;
   static constexpr bool TINY = TINY_;
   using lane_t = att_lane<W, TINY>;
   struct gathered { raw_t<T, W> k, v; };
@@ -144,7 +155,7 @@ struct att_fwd {
   }
   static __device__ __forceinline__ void row(const att_args& a, const lane_t& ln, const requested& o, row_t& w) {
 #pragma unroll
-    for (int r = 0; r < RQ; ++r) att_own<T, W, TINY>(o.q[r], ln, a.scale, w.q[r]);
+    for (int r = 0; r < RQ; ++r) att_own<T, W>(o.q[r], ln.scaled, w.q[r]);
   }
   template <int LPG>
   static __device__ __forceinline__ void edge(const att_args& a, const lane_t& ln, float bias, const gathered& g, const row_t& w, part (&s)[PARTS]) {
@@ -157,8 +168,10 @@ struct att_fwd {
     if (a.bias) {
       const bool out = bias == NEG_INF;
 #pragma unroll
-      for (int r = 0; r < RQ; ++r) z[r] = out ? NEG_INF : z[r] + bias;
-      if (__any(out)) {
+      for (int r = 0; r < RQ; ++r) z[r] += bias;
+      if (__any(out)) {  // (whatever their operands hold)
+#pragma unroll
+        for (int r = 0; r < RQ; ++r) z[r] = out ? NEG_INF : z[r];
 #pragma unroll
         for (int j = 0; j < W; ++j) v[j] = out ? 0.f : v[j];
       }
@@ -203,7 +216,7 @@ struct att_fwd {
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
       const int h = head(a, ln, r);
-      const float f = s[r].l == 0.f ? 0.f : 1.f / s[r].l;
+      const float f = att_inverse(s[r].l);
       float o[W];
 #pragma unroll
       for (int j = 0; j < W; ++j) o[j] = s[r].y[j] * f;
@@ -232,26 +245,26 @@ struct att_fwd {
 };
 
 // ---- backward ------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ float att_inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }  // (0: the row has nothing)
 // The numbers of a row and head that the columns' pass reads: reference, 1 / l, D.
 __device__ __forceinline__ void att_leave(const att_args& a, int row, int h, float d) {
   const int64_t at = (int64_t)row * a.heads + h;
-  a.stat[at] = make_float4(a.stats[2 * at], att_inverse(a.stats[2 * at + 1]), d, 0.f);
+  a.stat[at] = {a.stats[2 * at], att_inverse(a.stats[2 * at + 1]), d, 0.f};
 }
 // P of a score z whose row has numbers st
-__device__ __forceinline__ float att_weight(float z, const float4& st) { return fast_exp(z - st.x) * st.y; }
+__device__ __forceinline__ float att_weight(float z, const att_num& st) { return fast_exp(z - st.m) * st.inv; }
 
 // over A's rows: dq, and D
 template <class T_, int W_, int RQ_, bool TINY_>
 struct att_bwd_row {
   using T = T_;
-  static constexpr int W = W_, RQ = RQ_, RING = 4, PARTS = RQ;
+  static constexpr int W = W_, RQ = RQ_, RING = 4, PARTS = RQ, MOST = 2, WAVES = 1;
+  static constexpr bool WIDE = false;
   static constexpr bool TINY = TINY_;
   using lane_t = att_lane<W, TINY>;
   struct gathered { raw_t<T, W> k, v; };
   struct source { const T *k, *v; };
   struct requested { raw_t<T, W> q[RQ], dy[RQ]; float2 ml[RQ]; };
-  struct row_t { float q[RQ][W], dy[RQ][W]; float4 st[RQ]; };
+  struct row_t { float q[RQ][W], dy[RQ][W]; att_num st[RQ]; };
   struct part { float pt[W], p[W], d; };  // of a query head: sums of P t k, P k and P t
 
   static __device__ __forceinline__ int head(const att_args& a, const lane_t& ln, int r) { return ln.hk * a.group + (int)blockIdx.z * RQ + r; }
@@ -282,9 +295,9 @@ struct att_bwd_row {
   static __device__ __forceinline__ void row(const att_args& a, const lane_t& ln, const requested& o, row_t& w) {
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
-      att_own<T, W, TINY>(o.q[r], ln, a.scale, w.q[r]);
-      att_own<T, W, TINY>(o.dy[r], ln, 1.f, w.dy[r]);
-      w.st[r] = make_float4(o.ml[r].x, att_inverse(o.ml[r].y), 0.f, 0.f);
+      att_own<T, W>(o.q[r], ln.scaled, w.q[r]);
+      att_own<T, W>(o.dy[r], ln.own, w.dy[r]);
+      w.st[r] = {o.ml[r].x, att_inverse(o.ml[r].y), 0.f, 0.f};
     }
   }
   template <int LPG>
@@ -301,11 +314,13 @@ struct att_bwd_row {
     if (a.bias) {
       const bool out = bias == NEG_INF;
 #pragma unroll
-      for (int r = 0; r < RQ; ++r) {
-        z[r] = out ? NEG_INF : z[r] + bias;
-        z[RQ + r] = out ? 0.f : z[RQ + r];
-      }
+      for (int r = 0; r < RQ; ++r) z[r] += bias;
       if (__any(out)) {
+#pragma unroll
+        for (int r = 0; r < RQ; ++r) {
+          z[r] = out ? NEG_INF : z[r];
+          z[RQ + r] = out ? 0.f : z[RQ + r];
+        }
 #pragma unroll
         for (int j = 0; j < W; ++j) k[j] = out ? 0.f : k[j];
       }
@@ -368,11 +383,12 @@ __device__ __forceinline__ void att_out(const att_args& a, float* carry, T* out,
 template <class T_, int W_, int RQ_, bool TINY_>
 struct att_bwd_col {
   using T = T_;
-  static constexpr int W = W_, RQ = RQ_, RING = RQ == 1 ? 4 : 2, PARTS = 1;
+  static constexpr int W = W_, RQ = RQ_, RING = RQ == 1 ? 4 : 2, PARTS = 1, MOST = 4, WAVES = RQ == 4 ? 3 : 1;
+  static constexpr bool WIDE = false;
   static constexpr bool TINY = TINY_;
   using lane_t = att_lane<W, TINY>;
-  struct gathered { raw_t<T, W> q[RQ], dy[RQ]; float4 st[RQ]; };
-  struct source { const T *q, *dy; const float4* st; };
+  struct gathered { raw_t<T, W> q[RQ], dy[RQ]; att_num st[RQ]; };
+  struct source { const T *q, *dy; const att_num* st; };
   struct requested { raw_t<T, W> k, v; };
   struct row_t { float k[W], v[W]; };
   struct part { float dk[W], dv[W]; };
@@ -387,7 +403,7 @@ struct att_bwd_col {
   }
   static __device__ __forceinline__ void gather(const att_args& a, const source& o, int col, gathered& x) {
     const T *p = att_row<T>(o.q, col, a.pq), *d = att_row<T>(o.dy, col, a.pdy);
-    const float4* st = att_row<float4>(o.st, col, (uint32_t)a.heads * (uint32_t)sizeof(float4));
+    const att_num* st = att_row<att_num>(o.st, col, (uint32_t)a.heads * (uint32_t)sizeof(att_num));
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
       x.q[r] = att_load<T, W, TINY>(p + r * a.dh, a.dh);
@@ -401,8 +417,8 @@ struct att_bwd_col {
     o.v = att_load<T, W, TINY>(att_row<T>(a.v, row, a.pv) + at, a.dh);
   }
   static __device__ __forceinline__ void row(const att_args& a, const lane_t& ln, const requested& o, row_t& w) {
-    att_own<T, W, TINY>(o.k, ln, a.scale, w.k);
-    att_own<T, W, TINY>(o.v, ln, 1.f, w.v);
+    att_own<T, W>(o.k, ln.scaled, w.k);
+    att_own<T, W>(o.v, ln.own, w.v);
   }
   template <int LPG>
   static __device__ __forceinline__ void edge(const att_args& a, const lane_t& ln, float bias, const gathered& g, const row_t& w, part (&s)[PARTS]) {
@@ -418,11 +434,13 @@ struct att_bwd_col {
     if (a.bias) {
       const bool out = bias == NEG_INF;
 #pragma unroll
-      for (int r = 0; r < RQ; ++r) {
-        z[r] = out ? NEG_INF : z[r] + bias;
-        z[RQ + r] = out ? 0.f : z[RQ + r];
-      }
+      for (int r = 0; r < RQ; ++r) z[r] += bias;
       if (__any(out)) {
+#pragma unroll
+        for (int r = 0; r < RQ; ++r) {
+          z[r] = out ? NEG_INF : z[r];
+          z[RQ + r] = out ? 0.f : z[RQ + r];
+        }
 #pragma unroll
         for (int r = 0; r < RQ; ++r)
 #pragma unroll
@@ -434,7 +452,7 @@ struct att_bwd_col {
     }
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
-      const float p = att_weight(z[r], g.st[r]), ds = p * (z[RQ + r] - g.st[r].z);
+      const float p = att_weight(z[r], g.st[r]), ds = p * (z[RQ + r] - g.st[r].d);
 #pragma unroll
       for (int j = 0; j < W; ++j) {
         s[0].dk[j] = fmaf(ds, q[r][j], s[0].dk[j]);
@@ -485,7 +503,7 @@ struct att_bwd_col {
 
 // ---- a pass ----------------------------------------------------------------------------------------------------------
 template <class P, int LPG>
-__global__ void __launch_bounds__(ISP_WG) k_att(isp_view A, const int64_t* __restrict__ indptr, const int32_t* __restrict__ indices,
+__global__ void __launch_bounds__(ISP_WG, P::WAVES) k_att(isp_view A, const int64_t* __restrict__ indptr, const int32_t* __restrict__ indices,
                                                 const float* __restrict__ bias, att_args a) {
   __shared__ rn_lds lds;
   constexpr int G = ISP_WAVE / LPG, RING = P::RING, CHUNK = RING % 4 == 0 ? 2 : 1;
@@ -527,11 +545,13 @@ __global__ void __launch_bounds__(ISP_WG) k_att(isp_view A, const int64_t* __res
         [&](auto u, float b, int) { P::template edge<LPG>(a, ln, b, x[u], cur, st); },
         [&](int k, int row) {
           if (!carried) P::store(a, ln, row, st);
+          if (__any(carried)) {  // (once per run)
 #pragma unroll
-          for (int i = 0; i < PARTS; ++i) {
-            if (carried) head[i] = st[i];
-            P::clear(st[i]);
+            for (int i = 0; i < PARTS; ++i)
+              if (carried) head[i] = st[i];
           }
+#pragma unroll
+          for (int i = 0; i < PARTS; ++i) P::clear(st[i]);
           carried = false;
           ended = true;
           P::row(a, ln, next, cur);
@@ -625,7 +645,7 @@ __global__ void __launch_bounds__(ISP_WG) k_att_fwd_fixup(isp_view A, att_args a
     l = fmaf(part[i][1][lane], f, l);
     y = fmaf(part[i][2][lane], f, y);
   }
-  static_cast<T*>(a.y)[(int64_t)row * a.ldy + col] = (T)(l == 0.f ? 0.f : y / l);
+  static_cast<T*>(a.y)[(int64_t)row * a.ldy + col] = (T)(y * att_inverse(l));
   if (a.stats && col == h * a.dh) {
     float* st = a.stats + ((int64_t)row * a.heads + h) * 2;
     st[0] = m;
@@ -699,7 +719,8 @@ isp_status att_launch(const isp_view& v, const att_args& a, int chunks, hipStrea
 // Lanes to a group: as many of the heads as 64 lanes hold.
 template <template <class, int, int, bool> class P, class T, int W, int RQ>
 isp_status att_lanes(const isp_view& v, const att_args& a, int chunks, hipStream_t s) {
-  if (a.dh < W) return att_launch<P<T, W, RQ, true>, 4>(v, a, chunks, s);
+  if constexpr (W == 4)
+    if (a.dh < W) return att_launch<P<T, W, RQ, true>, 4>(v, a, chunks, s);
   int lanes = 4;
   while (lanes < ISP_WAVE && lanes < a.lph * a.kv_heads) lanes *= 2;
   switch (lanes) {
@@ -711,8 +732,12 @@ isp_status att_lanes(const isp_view& v, const att_args& a, int chunks, hipStream
   }
 }
 template <template <class, int, int, bool> class P, class T>
-isp_status att_pass(const isp_view& v, const att_args& a, int rq, int chunks, hipStream_t s) {
-  if (rq == 4) return att_lanes<P, T, 4, 4>(v, a, chunks, s);
+isp_status att_pass(const isp_view& v, att_args a, int rq, int chunks, bool wide, hipStream_t s) {
+  a.lph = att_lanes_per_head(a.dh, wide ? 8 : 4);
+  if constexpr (P<T, 4, 1, false>::WIDE)
+    if (wide) return att_lanes<P, T, 8, 1>(v, a, chunks, s);
+  if constexpr (P<T, 4, 1, false>::MOST == 4)
+    if (rq == 4) return att_lanes<P, T, 4, 4>(v, a, chunks, s);
   if (rq == 2) return att_lanes<P, T, 4, 2>(v, a, chunks, s);
   return att_lanes<P, T, 4, 1>(v, a, chunks, s);
 }
@@ -720,8 +745,9 @@ isp_status att_pass(const isp_view& v, const att_args& a, int rq, int chunks, hi
 template <class T>
 isp_status att_forward(const isp_csr* A, att_args a, hipStream_t s) {
   const isp_view& v = A->v;
-  const int rq = att_share(a.group);
-  isp_status st = att_pass<att_fwd, T>(v, a, rq, a.group / rq, s);
+  const int rq = att_share(a.group, 4);
+  isp_status st = att_pass<att_fwd, T>(v, a, rq, a.group / rq,
+                                     att_wide(sizeof(T), a.group, a.kv_heads, a.dh, A->info.nnz, A->info.n_rows - A->info.bin_rows[0]), s);
   if (st != ISP_OK || v.n_hub == 0) return st;
   k_att_fwd_fixup<T><<<dim3((unsigned)v.n_hub, (unsigned)((a.heads * a.dh + ISP_WAVE - 1) / ISP_WAVE)), ISP_WG, 0, s>>>(v, a);
   ISP_LAUNCH_CHECK();
@@ -731,10 +757,10 @@ isp_status att_forward(const isp_csr* A, att_args a, hipStream_t s) {
 template <class T>
 isp_status att_backward(const isp_csr* A, att_args a, const att_grads& o, hipStream_t s) {
   const isp_view &v = A->v, &vt = A->At ? A->At->v : A->v;
-  const int rq = att_share(a.group), passes = a.group / rq;
+  const int rq_row = att_share(a.group, 2), rq = att_share(a.group, 4), passes = a.group / rq;
   a.y = o.dq;
   a.ldy = o.lddq;
-  isp_status st = att_pass<att_bwd_row, T>(v, a, rq, passes, s);
+  isp_status st = att_pass<att_bwd_row, T>(v, a, rq_row, a.group / rq_row, false, s);
   if (st != ISP_OK) return st;
   if (v.n_hub > 0) {
     k_att_row_fixup<T><<<dim3((unsigned)v.n_hub, (unsigned)((a.heads * a.dh + ISP_WAVE - 1) / ISP_WAVE)), ISP_WG, 0, s>>>(v, a);
@@ -747,7 +773,7 @@ isp_status att_backward(const isp_csr* A, att_args a, const att_grads& o, hipStr
   a.ldy2 = o.lddv;
   a.passes = passes;
   for (a.pass = 0; a.pass < passes; ++a.pass) {
-    if ((st = att_pass<att_bwd_col, T>(vt, a, rq, 1, s)) != ISP_OK) return st;
+    if ((st = att_pass<att_bwd_col, T>(vt, a, rq, 1, false, s)) != ISP_OK) return st;
     if (vt.n_hub > 0) {
       k_att_col_fixup<T><<<dim3((unsigned)vt.n_hub, (unsigned)((2 * a.kv_heads * a.dh + ISP_WAVE - 1) / ISP_WAVE)), ISP_WG, 0, s>>>(vt, a);
       ISP_LAUNCH_CHECK();

@@ -49,10 +49,10 @@ struct backward_space {  // (offsets)
 backward_space backward_bytes(const isp_csr* A, int32_t heads, int32_t kv_heads, int32_t dh) {
   backward_space b;
   const int group = heads / kv_heads;
-  b.part = isp_align((size_t)A->v.n_rows * heads * sizeof(float4));
+  b.part = isp_align((size_t)A->v.n_rows * heads * sizeof(att_num));
   const size_t row = (size_t)A->v.n_seg * heads * (2 * dh + 1), col = A->At ? (size_t)A->At->v.n_seg * 2 * kv_heads * dh : 0;
   b.carry = b.part + isp_align((row > col ? row : col) * sizeof(float));
-  const size_t carry = group > att_share(group) ? isp_align((size_t)A->v.n_cols * kv_heads * dh * sizeof(float)) : 0;
+  const size_t carry = group > isp_dev::att_share(group, 4) ? isp_align((size_t)A->v.n_cols * kv_heads * dh * sizeof(float)) : 0;
   b.carry2 = b.carry + carry;
   b.total = b.carry2 + carry;
   return b;
@@ -64,8 +64,6 @@ att_args make_args(int32_t heads, int32_t kv_heads, int32_t dh, float scale, uns
   a.kv_heads = kv_heads;
   a.group = heads / kv_heads;
   a.dh = dh;
-  a.lph = 1;
-  while (a.lph * 4 < dh) a.lph *= 2;
   a.scale = scale;
   a.bias = (flags & ISP_BIAS_BY_A) != 0;
   a.passes = 1;
@@ -142,7 +140,7 @@ isp_status isp_attention_backward(const isp_csr_t* A, const void* Q, int64_t ldq
   a.q = Q, a.k = K, a.v = V, a.dy = dY;
   a.pq = (uint32_t)ldq * size, a.pk = (uint32_t)ldk * size, a.pv = (uint32_t)ldv * size, a.pdy = (uint32_t)lddy * size;
   a.stats = const_cast<float*>(stats);
-  a.stat = reinterpret_cast<float4*>(ws);
+  a.stat = reinterpret_cast<att_num*>(ws);
   a.part = reinterpret_cast<float*>(ws + b.part);
   a.carry = reinterpret_cast<float*>(ws + b.carry);
   a.carry2 = reinterpret_cast<float*>(ws + b.carry2);

@@ -1,9 +1,16 @@
 // What the passes of the attention over a CSR matrix take (attention.h), and how its entry points (attention.hip) reach them.
 #pragma once
+#include "attention_rule.h"
 #include "isp_internal.h"
 
 constexpr int ATT_MAX_DIM = 256;     // columns of a head: 64 lanes of four
 constexpr int ATT_MAX_HEADS = 4096;
+
+// What the columns' pass of the backward reads of a row and head: the reference of its scores, 1 / (the sum of exp(s - m)), D.  16 bytes: eight heads'
+// are one line (12: 169 k rows, 2.4 M entries, 8 heads of 16, fp32 288 / 299 us).
+struct __attribute__((aligned(16))) att_num {
+  float m, inv, d, spare;
+};
 
 struct att_args {
   const void *q, *k, *v, *dy;
@@ -15,7 +22,7 @@ struct att_args {
   void *y, *y2;              // output rows (forward y, backward dq or dk; y2: dv)
   int64_t ldy, ldy2;         // in elements
   float* stats;              // (m, l) per row and head: written by the forward (may be NULL), read by the backward
-  float4* stat;              // backward: (m, 1 / l, D, -) per row and head, in the workspace
+  att_num* stat;             // backward, per row and head, in the workspace
   float* part;               // partial rows of the split rows' segments, in the workspace
   float *carry, *carry2;     // dk and dv between the passes over a key head's query heads, fp32, rows of kv_heads * dh, in the workspace
   int pass, passes;
@@ -24,9 +31,6 @@ struct att_grads {
   void *dq, *dk, *dv;
   int64_t lddq, lddk, lddv;
 };
-
-// Query heads of a key head that a lane takes at once: as many of four as divide them.
-inline int att_share(int group) { return group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1; }
 
 isp_status isp_att_forward_f32(const isp_csr* A, const att_args& a, hipStream_t s);
 isp_status isp_att_forward_bf16(const isp_csr* A, const att_args& a, hipStream_t s);

@@ -1,0 +1,30 @@
+// How the attention's passes share the heads out over lanes (attention.h): host arithmetic only, so that the rules can be checked without a device.
+#pragma once
+#include <stdint.h>
+
+namespace isp_dev {
+
+// Lanes that hold a head of dh columns, w of them to a lane: a power of two, for the sums over them.
+inline int att_lanes_per_head(int dh, int w) {
+  int l = 1;
+  while (l * w < dh) l *= 2;
+  return l;
+}
+
+// Query heads of a key head that a lane takes at once: as many of `most` (4 or 2) as divide them.  The forward and the columns' pass take four, which reads
+// the gathered rows once for all; the rows' pass two, as four of them need 230 registers.  us with four / two, 1 M rows, 17 M entries, 8 query
+// heads on 2 of 16, bf16: forward 720 / 884, rows 1507 / 1487, columns 1294 / 2364 (in two passes).
+inline int att_share(int group, int most) { return group % 4 == 0 && most == 4 ? 4 : group % 2 == 0 ? 2 : 1; }
+
+// The forward of 16-bit operands with one query head to a key head gives a lane eight columns instead of four where that leaves eight lanes to a
+// group and rows average 16 entries: half the lanes, so twice the entries per step, and half the exponentials, for 40 registers more.
+// us with four / eight, bf16: R-MAT, 169 k rows, 2.4 M entries: 8 heads of 8 68.6 / 60.9, 8 of 16 121 / 113, 3 of 20 114 / 96, 1 of 64 70 / 60; 60 k, 6 M: 8 of 16 236 / 169, 2 of 128 531 / 349,
+// 2 of 50 250 / 192; 1 M, 17 M: 8 of 16 821 / 807; 20 k, 400 k: 3 of 20 31.2 / 25.0; four lanes to a group: 169 k, 2.4 M: 2 of 16 52.1 / 53.9; uniform, 10 entries a row, 100 k, 1 M: 8 of 8
+// 47.3 / 49.0, 4 of 32 87.4 / 90.2.  The backward's passes keep four: their registers are the limit (8 of 16 on 2.4 M entries: rows 151 / 184, columns 176 / 176), and so do fp32
+// operands, which wait for their gathers (8 of 16 251 / 251, 8 of 8 110 / 112; 60 k, 6 M: 8 of 16 334 / 351, 1 of 64 157 / 170).
+// live_rows: rows with entries.
+inline bool att_wide(int element_bytes, int group, int kv_heads, int dh, int64_t nnz, int64_t live_rows) {
+  return element_bytes == 2 && group == 1 && dh >= 8 && att_lanes_per_head(dh, 8) * kv_heads >= 5 && nnz >= 16 * live_rows;
+}
+
+}  // namespace isp_dev
