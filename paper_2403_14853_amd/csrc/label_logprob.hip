@@ -47,14 +47,32 @@ __device__ __forceinline__ float from_order_bits(unsigned k) {
   return __uint_as_float(k == 0xffffffffu ? 0x7fc00000u : k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
 __device__ __forceinline__ u64 key_of(unsigned bits, int index) { return (u64)bits << 32 | (unsigned)~index; }
+__device__ __forceinline__ unsigned max_u(unsigned a, unsigned b) { return a > b ? a : b; }
+template <int CTRL>
+__device__ __forceinline__ unsigned dpp_u(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true); }
+// The maximum over LPR consecutive lanes (4 and more), in all of them.
+template <int LPR>
+__device__ __forceinline__ unsigned lanes_max_u(unsigned v) {
+  v = max_u(v, dpp_u<DPP_XOR1>(v));
+  v = max_u(v, dpp_u<DPP_XOR2>(v));
+  if constexpr (LPR >= 8) v = max_u(v, dpp_u<DPP_HALF_MIRROR>(v));
+  if constexpr (LPR >= 16) v = max_u(v, dpp_u<DPP_ROR8>(v));
+  if constexpr (LPR >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max_u(r[0], r[1]);
+  }
+  if constexpr (LPR >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = max_u(r[0], r[1]);
+  }
+  return v;
+}
+// of keys: the greatest score first, then, among the lanes that have it, the lowest index
 template <int LPR>
 __device__ __forceinline__ u64 lanes_max_key(u64 k) {
-#pragma unroll
-  for (int o = 1; o < LPR; o <<= 1) {
-    const u64 t = __shfl_xor(k, o);
-    k = t > k ? t : k;
-  }
-  return k;
+  const unsigned hi = lanes_max_u<LPR>((unsigned)(k >> 32));
+  const unsigned lo = lanes_max_u<LPR>((unsigned)(k >> 32) == hi ? (unsigned)k : 0u);
+  return (u64)hi << 32 | lo;
 }
 
 // The running sums of some scores: m their maximum (-inf: none counts yet).
@@ -72,13 +90,10 @@ __device__ __forceinline__ lp_sums lp_join(const lp_sums& a, const lp_sums& b) {
   const lp_sums x = lp_rescale(a, m), y = lp_rescale(b, m);
   return {m, x.t + y.t, x.u + y.u};
 }
+// scores of at most s.m
 template <int N>
-__device__ __forceinline__ void lp_add(lp_sums& s, const float (&z)[N]) {
-  float m = s.m;
-#pragma unroll
-  for (int c = 0; c < N; ++c) m = fmaxf(m, z[c]);
-  s = lp_rescale(s, m);
-  const float base = m == NEG_INF ? 0.f : m;
+__device__ __forceinline__ void lp_add_to(lp_sums& s, const float (&z)[N]) {
+  const float base = s.m == NEG_INF ? 0.f : s.m;
   float t[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};  // (short sums first: a long row's errors stay small)
 #pragma unroll
   for (int c = 0; c < N; ++c) {
@@ -89,11 +104,21 @@ __device__ __forceinline__ void lp_add(lp_sums& s, const float (&z)[N]) {
   s.t += (t[0] + t[1]) + (t[2] + t[3]);
   s.u += (u[0] + u[1]) + (u[2] + u[3]);
 }
+template <int N>
+__device__ __forceinline__ void lp_add(lp_sums& s, const float (&z)[N]) {
+  float m = s.m;
+#pragma unroll
+  for (int c = 0; c < N; ++c) m = fmaxf(m, z[c]);
+  s = lp_rescale(s, m);
+  lp_add_to(s, z);
+}
 
+constexpr float LN2 = 0.693147180559945309f;
+// (the hardware's base-2 logarithm and reciprocal, about 1 ulp each: t is 1 or more)
 struct lp_row {
   float m, log_t;
   bool empty;
-  __device__ __forceinline__ lp_row(const lp_sums& s) : m(s.m), log_t(logf(s.t)), empty(s.t == 0.f) {}
+  __device__ __forceinline__ lp_row(const lp_sums& s) : m(s.m), log_t(__builtin_amdgcn_logf(s.t) * LN2), empty(s.t == 0.f) {}
   __device__ __forceinline__ float logprob(float z) const { return empty ? NEG_INF : (z - m) - log_t; }
 };
 // one lane per row
@@ -103,7 +128,7 @@ __device__ __forceinline__ void lp_store(const lp_args& a, int64_t row, const lp
     const int64_t y = a.labels[row];
     a.logprob[row] = y >= 0 && y < a.classes ? r.logprob((float)static_cast<const T*>(a.z)[row * a.ldz + y]) : 0.f;
   }
-  if (a.entropy) a.entropy[row] = r.empty ? 0.f : r.log_t - s.u / s.t;
+  if (a.entropy) a.entropy[row] = r.empty ? 0.f : r.log_t - s.u * __builtin_amdgcn_rcpf(s.t);
   if (a.stats) {
     a.stats[2 * row] = r.m;
     a.stats[2 * row + 1] = r.log_t;
@@ -137,7 +162,7 @@ __global__ void __launch_bounds__(ISP_WG) k_lp_group(lp_args a) {
       }
     }
     lp_sums s{lanes_max<LPR>(m), 0.f, 0.f};
-    lp_add(s, z);
+    lp_add_to(s, z);
     s.t = lanes_sum<LPR>(s.t);
     s.u = lanes_sum<LPR>(s.u);
     const lp_row r(s);
@@ -176,43 +201,59 @@ __global__ void __launch_bounds__(ISP_WG) k_lp_group(lp_args a) {
 // The best keys that a wavefront has met, in order: lane i holds the i-th (0: none yet).
 struct lp_list {
   u64 key = 0;
-  __device__ __forceinline__ u64 last(int top) const { return __shfl(key, top - 1); }
+  __device__ __forceinline__ u64 last(int top) const {  // (top is wave-uniform)
+    const unsigned hi = (unsigned)__builtin_amdgcn_readlane((int)(key >> 32), top - 1), lo = (unsigned)__builtin_amdgcn_readlane((int)key, top - 1);
+    return (u64)hi << 32 | lo;
+  }
   __device__ __forceinline__ void insert(u64 x, int lane) {
     const u64 before = __shfl_up(key, 1);
     key = key > x ? key : lane == 0 || before > x ? x : before;
   }
-  // one key per lane
-  __device__ __forceinline__ void merge(u64 mine, int top, int lane) {
+  // N keys per lane
+  template <int N>
+  __device__ __forceinline__ void merge(u64 (&mine)[N], int top, int lane) {
     for (;;) {
-      const u64 best = lanes_max_key<ISP_WAVE>(mine);
+      u64 m = mine[0];
+#pragma unroll
+      for (int i = 1; i < N; ++i) m = mine[i] > m ? mine[i] : m;
+      const u64 best = lanes_max_key<ISP_WAVE>(m);
       if (best <= last(top)) break;
       insert(best, lane);
-      if (mine == best) mine = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) mine[i] = mine[i] == best ? 0 : mine[i];
     }
   }
 };
 
+// A tile as it lies in memory: scores behind the row's end as -inf.
 template <class T>
-__device__ __forceinline__ void lp_load_tile(const T* p, int at, int end, int lane, float (&z)[16]) {
-  constexpr int VEC = 16 / sizeof(T), NV = 16 / VEC;
-  if (at + LP_TILE <= end) {
+struct lp_tile {
+  static constexpr int VEC = 16 / sizeof(T), NV = 16 / VEC;
+  raw_t<T, VEC> raw[NV];
+  __device__ __forceinline__ void load(const T* p, int at, int end, int lane) {
+    if (at + LP_TILE <= end) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) raw[v] = load_raw<T, VEC>(p + at + (v * ISP_WAVE + lane) * VEC);
+    } else {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int c = 0; c < VEC; ++c) {
+          const int i = at + (v * ISP_WAVE + lane) * VEC + c;
+          raw[v][c] = i < end ? p[i] : (T)NEG_INF;
+        }
+    }
+  }
+  __device__ __forceinline__ void get(float (&z)[16]) const {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       float t[VEC];
-      to_float<T, VEC>(load_raw<T, VEC>(p + at + (v * ISP_WAVE + lane) * VEC), t);
+      to_float<T, VEC>(raw[v], t);
 #pragma unroll
       for (int c = 0; c < VEC; ++c) z[v * VEC + c] = t[c];
     }
-  } else {
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int c = 0; c < VEC; ++c) {
-        const int i = at + (v * ISP_WAVE + lane) * VEC + c;
-        z[v * VEC + c] = i < end ? (float)p[i] : NEG_INF;
-      }
   }
-}
+};
 
 // WPR wavefronts to a row: 1, or all of the workgroup's.
 template <class T, int WPR, bool TOP>
@@ -220,25 +261,35 @@ __global__ void __launch_bounds__(LP_WAVES* ISP_WAVE) k_lp_stream(lp_args a) {
   constexpr int VEC = 16 / sizeof(T);
   __shared__ float sums[LP_WAVES][3];
   __shared__ u64 keys[LP_WAVES][ISP_WAVE];
+  __shared__ unsigned floor_bits;
   const int lane = threadIdx.x & (ISP_WAVE - 1), w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int64_t row = WPR == 1 ? (int64_t)blockIdx.x * LP_WAVES + w : (int64_t)(blockIdx.x / (unsigned)a.splits);
   if (row >= a.n) return;  // (the whole workgroup, or a wavefront that meets no barrier)
   const T* p = static_cast<const T*>(a.z) + row * a.ldz;
   const int first = WPR == 1 ? 0 : (int)(blockIdx.x % (unsigned)a.splits) * LP_WAVES + w, stride = WPR == 1 ? 1 : a.splits * LP_WAVES;
   const int tiles = (a.classes + LP_TILE - 1) / LP_TILE;
+  if constexpr (TOP && WPR > 1) {
+    if (threadIdx.x == 0) floor_bits = 0u;
+    __syncthreads();
+  }
   lp_sums s{NEG_INF, 0.f, 0.f};
   lp_list list;
   unsigned last = 0;  // the score bits of the list's last key
+  lp_tile<T> next;
+  if (first < tiles) next.load(p, first * LP_TILE, a.classes, lane);
   for (int tile = first; tile < tiles; tile += stride) {
     float z[16];
-    lp_load_tile<T>(p, tile * LP_TILE, a.classes, lane, z);
+    next.get(z);
+    if (tile + stride < tiles) next.load(p, (tile + stride) * LP_TILE, a.classes, lane);  // (on its way while this one is worked on)
     lp_add(s, z);
     if constexpr (TOP) {
       float m = NEG_INF;
 #pragma unroll
       for (int c = 0; c < 16; ++c) m = fmaxf(m, z[c]);
+      const unsigned low = WPR > 1 ? __hip_atomic_load(&floor_bits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) : 0u;  // (what a wavefront of the row has `top` keys from is enough for all of them)
+      const unsigned mb = order_bits(m);
       // (s.t: once a NaN has come by every tile is looked at)
-      if (__any(last == 0 || order_bits(m) > last || s.t != s.t)) {
+      if (__any((mb > last && mb >= low) || s.t != s.t)) {
         unsigned bits[16];
 #pragma unroll
         for (int c = 0; c < 16; ++c) {
@@ -246,23 +297,24 @@ __global__ void __launch_bounds__(LP_WAVES* ISP_WAVE) k_lp_stream(lp_args a) {
           bits[c] = i < a.classes ? order_bits(z[c]) : 0u;
         }
         for (;;) {
-          u64 mine = 0;
+          unsigned mine = bits[0];
 #pragma unroll
-          for (int c = 0; c < 16; ++c) {
-            const u64 key = bits[c] ? key_of(bits[c], tile * LP_TILE + (c / VEC * ISP_WAVE + lane) * VEC + c % VEC) : 0;
-            mine = key > mine ? key : mine;
-          }
-          const u64 best = lanes_max_key<ISP_WAVE>(mine);
-          if (best <= list.last(a.top)) break;
-          list.insert(best, lane);
-          if (mine == best) {
-            const int at = (int)~(unsigned)best;
+          for (int c = 1; c < 16; ++c) mine = max_u(mine, bits[c]);
+          const unsigned hi = lanes_max_u<ISP_WAVE>(mine);
+          if (hi == 0 || hi <= last || hi < low) break;  // (later scores that equal the list's last come after it)
+          int at = 0;
 #pragma unroll
-            for (int c = 0; c < 16; ++c)
-              if (tile * LP_TILE + (c / VEC * ISP_WAVE + lane) * VEC + c % VEC == at) bits[c] = 0;
+          for (int c = 15; c >= 0; --c) at = bits[c] == hi ? c : at;
+          const int index = tile * LP_TILE + (at / VEC * ISP_WAVE + lane) * VEC + at % VEC;
+          const unsigned lo = lanes_max_u<ISP_WAVE>(mine == hi ? (unsigned)~index : 0u);
+          list.insert((u64)hi << 32 | lo, lane);
+          last = (unsigned)(list.last(a.top) >> 32);
+          if (mine == hi && (unsigned)~index == lo) {
+#pragma unroll
+            for (int c = 0; c < 16; ++c) bits[c] = c == at ? 0u : bits[c];
           }
         }
-        last = (unsigned)(list.last(a.top) >> 32);
+        if (WPR > 1 && lane == 0 && last > low) atomicMax(&floor_bits, last);
       }
     }
   }
@@ -282,10 +334,18 @@ __global__ void __launch_bounds__(LP_WAVES* ISP_WAVE) k_lp_stream(lp_args a) {
     if constexpr (TOP) keys[w][lane] = lane < a.top ? list.key : 0;
     __syncthreads();
     if (w > 0) return;
+    // (eight lanes have a wavefront's sums each, the others nothing)
+    s = lane < LP_WAVES ? lp_sums{sums[lane][0], sums[lane][1], sums[lane][2]} : lp_sums{NEG_INF, 0.f, 0.f};
+    const float m = lanes_max<ISP_WAVE>(s.m);
+    s = lp_rescale(s, m);
+    s.t = lanes_sum<ISP_WAVE>(s.t);
+    s.u = lanes_sum<ISP_WAVE>(s.u);
+    if constexpr (TOP) {
+      u64 mine[LP_WAVES];
 #pragma unroll
-    for (int i = 1; i < LP_WAVES; ++i) {
-      s = lp_join(s, {sums[i][0], sums[i][1], sums[i][2]});
-      if constexpr (TOP) list.merge(keys[i][lane], a.top, lane);
+      for (int i = 0; i < LP_WAVES; ++i) mine[i] = keys[i][lane];
+      list = lp_list();
+      list.merge(mine, a.top, lane);
     }
     if (a.splits > 1) {
       float* o = a.part + 3 * (int64_t)blockIdx.x;
@@ -324,7 +384,12 @@ __global__ void __launch_bounds__(ISP_WAVE) k_lp_join(lp_args a) {
     const u64* k = reinterpret_cast<const u64*>(a.part + (3 * a.n * a.splits + 1) / 2 * 2) + row * a.splits * a.top;
     lp_list list;
     const int n = a.splits * a.top;
-    for (int i = 0; i < n; i += ISP_WAVE) list.merge(i + lane < n ? k[i + lane] : 0, a.top, lane);
+    for (int i = 0; i < n; i += 4 * ISP_WAVE) {
+      u64 mine[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) mine[j] = i + j * ISP_WAVE + lane < n ? k[i + j * ISP_WAVE + lane] : 0;
+      list.merge(mine, a.top, lane);
+    }
     if (lane < a.top) lp_store_top(a, row, lane, list.key, r);
   }
 }
