@@ -50,6 +50,9 @@ def main():
     ap.add_argument("--gcn-step", action="store_true",
                     help="instead of the benchmark line: a 2-layer GCN training step (sparse ops through the "
                          "autograd wrappers, dense GEMMs through torch) with hidden width d")
+    ap.add_argument("--attention-step", action="store_true",
+                    help="instead of the benchmark line: the training step of a node classifier with one attention layer (layer norm, attention over the "
+                         "graph, layer norm, log probabilities of 47 classes' labels; dense GEMMs through torch) in fp32 and bf16")
     ap.add_argument("--reductions", action="store_true",
                     help="instead of the benchmark line: forward and backward time of the mean / min / max reductions")
     ap.add_argument("--flushed", action="store_true",
@@ -122,6 +125,9 @@ def main():
         return
     if args.gcn_step:
         print(json.dumps(gcn_step(w, indptr, indices, values, X)))
+        return
+    if args.attention_step:
+        print(json.dumps(attention_step(w, indptr, indices, X)))
         return
 
     ops = list(w.ops)
@@ -497,6 +503,39 @@ def gcn_step(w, indptr, indices, values, X):
     return {"what": "2-layer GCN training step (4 SpMM + 6 GEMM + elementwise)", "workload": w.name, "hidden": d,
             "ms_per_step": round(ms, 3), "sparse_flops": 4 * 2.0 * w.nnz * d,
             "sparse_gflops_if_all_time_were_sparse": round(4 * 2.0 * w.nnz * d / ms / 1e6, 1)}
+
+
+def attention_step(w, indptr, indices, X, classes=47):
+    """A node classifier's step: h = X + attention(norm(X) Wq, norm(X) Wk, norm(X) Wv), scores = norm(h) Wo, the loss the labels' mean negative log
+    probability, backward, SGD update.  Heads of 16 columns (one head where the width is no multiple of that)."""
+    import torch
+    from paper_2403_14853_amd import autograd as ag
+    g = ag.SparseGraph(indptr, indices)
+    d = w.d
+    heads = d // 16 if d % 16 == 0 else 1
+    out = {"what": "training step of a node classifier with one attention layer (2 layer norms, attention, log probabilities, 12 GEMMs, elementwise)",
+           "workload": w.name, "hidden": d, "heads": heads, "classes": classes, "ms_per_step": {}}
+    for name, dtype in (("f32", torch.float32), ("bf16", torch.bfloat16)):
+        torch.manual_seed(0)
+        x = X.to(dtype)
+        weights = [(torch.randn(d, k, device="cuda") / d ** 0.5).to(dtype).requires_grad_(True) for k in (d, d, d, classes)]
+        norms = [torch.full((d,), v, device="cuda").requires_grad_(True) for v in (1.0, 0.0, 1.0, 0.0)]
+        labels = torch.randint(-1, classes, (w.n,), device="cuda")
+
+        def step():
+            h = ag.layer_norm(x, *norms[:2])
+            h = x + ag.attention(g, h @ weights[0], h @ weights[1], h @ weights[2], heads)
+            loss = -ag.label_logprob(ag.layer_norm(h, *norms[2:]) @ weights[3], labels)[0].mean()
+            loss.backward()
+            with torch.no_grad():
+                for p in weights + norms:
+                    p -= 1e-3 * p.grad
+                    p.grad = None
+
+        step()
+        step()
+        out["ms_per_step"][name] = round(_time_ms(step, 10), 3)
+    return out
 
 
 def reductions(isp, w, A, X, dY):
