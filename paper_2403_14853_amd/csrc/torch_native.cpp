@@ -1074,6 +1074,7 @@ struct AttentionBackward : torch::autograd::Node {
   Heads H{};
   float scale = 0.f;
   unsigned flags = 0;
+  uint32_t bias_version = 0;  // of the graph's values, where they take part
   std::string name() const override { return "IspAttentionBackward"; }
   void release_variables() override {
     for (SavedVariable* v : {&Q, &K, &V}) v->reset_data();
@@ -1083,6 +1084,8 @@ struct AttentionBackward : torch::autograd::Node {
     variable_list out(3);
     if (!grads[0].defined()) return out;
     at::NoGradGuard no_grad;
+    TORCH_CHECK(!(flags & ISP_BIAS_BY_A) || graph->values._version() == bias_version,
+                "the graph's values, which the attention's backward needs, have been modified by an inplace operation");
     const Tensor q = Q.unpack(), k = K.unpack(), v = V.unpack(), dY = rows_of(grads[0]);
     const bool rows = task_should_compute_output(0), cols = task_should_compute_output(1) || task_should_compute_output(2);
     if (cols) transpose(*graph);
@@ -1162,6 +1165,7 @@ PyObject* py_ag_attention(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
       node->H = H;
       node->scale = (float)scale;
       node->flags = flags;
+      if (flags & ISP_BIAS_BY_A) node->bias_version = g->version;
       torch::autograd::set_history(Y, node);
     }
   }

@@ -417,6 +417,12 @@ def test_autograd(dtype):
     y = ag.attention(g, *leaves, heads, kv, bias=True)
     for t, name in zip(torch.autograd.grad(y, leaves, dy), ("dq", "dk", "dv")):
         check(t, reference(indptr, cols, q, k, v, dy, heads, kv, c ** -0.5, 2 * bias), name)
+    y, plain = ag.attention(g, *leaves, heads, kv, bias=True), ag.attention(g, *leaves, heads, kv)
+    with torch.no_grad():
+        g.values.mul_(2)
+    with pytest.raises(RuntimeError):  # (the backward needs the bias of the forward)
+        y.backward(dy)
+    check(torch.autograd.grad(plain, leaves, dy)[0], reference(indptr, cols, q, k, v, dy, heads, kv, c ** -0.5), "dq")
     x = q.clone().requires_grad_(True)
     w = x * 1
     y = ag.attention(g, w, k, v, heads, kv)

@@ -1,0 +1,169 @@
+"""Calls of the attention and the row-wise operators that their own files' sizes do not reach: operands beyond 4 GB, offsets beyond 32 bits, forced small
+work partitions, shared transposes, aliasing-free slices of one buffer, parameters left out."""
+import os
+
+import numpy as np
+import pytest
+import torch
+
+import graphgen
+import paper_2403_14853_amd as isp
+from paper_2403_14853_amd import autograd as ag
+import test_gpu_attention as att
+import test_gpu_label_logprob as lab
+import test_gpu_layer_norm as norm
+
+pytestmark = pytest.mark.gpu
+
+
+def with_env(env, f):
+    old = {k: os.environ.get(k) for k in env}
+    os.environ.update(env)
+    try:
+        return f()
+    finally:
+        for k, v in old.items():
+            if v is None:
+                os.environ.pop(k, None)
+            else:
+                os.environ[k] = v
+
+
+@pytest.mark.parametrize("env", [dict(ISP_HUB_THRESHOLD="8", ISP_SEGMENT_LEN="8", ISP_BLOCK_COST="16"), dict(ISP_HUB_THRESHOLD="512", ISP_SEGMENT_LEN="768", ISP_BLOCK_COST="256"),
+                                 dict(ISP_HUB_THRESHOLD="64", ISP_SEGMENT_LEN="100", ISP_BLOCK_COST="256", ISP_BANDS="4"), dict(ISP_NO_GROUPED="1")],
+                         ids=["tiny", "largest", "bands", "general"])
+@pytest.mark.parametrize("heads,kv,c,dtype", [(4, 4, 16, torch.float32), (8, 2, 12, torch.bfloat16), (3, 3, 20, torch.float16), (2, 1, 3, torch.float32), (1, 1, 256, torch.float16)])
+def test_forced_partitions(env, heads, kv, c, dtype):
+    n, m = 260, 240
+    indptr, cols = att.graph(n, m, 21)
+    bias = torch.randn(len(cols), generator=torch.Generator().manual_seed(1))
+    bias[::7] = -np.inf
+    q, k, v, dy = att.operands(n, m, heads, kv, c, dtype)
+    A = with_env(env, lambda: att.build(indptr, cols, m, bias))
+    att.check_all(att.run(A, q, k, v, dy, heads, kv, bias=True), att.reference(indptr, cols, q, k, v, dy, heads, kv, c ** -0.5, bias))
+
+
+def test_shared_transpose_of_a_large_symmetric_pattern():
+    """(More than 4 Mi entries: the transpose shares the matrix's partitions; the values differ between an entry and its mirror.)"""
+    n = 40_000
+    gen = np.random.default_rng(0)
+    u, v = gen.integers(0, n, 2_400_000), gen.integers(0, n, 2_400_000)
+    u[:300_000] = 17  # a long row and column
+    keys = np.unique(np.concatenate([u * n + v, v * n + u]))
+    indptr = torch.from_numpy(np.searchsorted(keys // n, np.arange(n + 1)).astype(np.int64))
+    cols = torch.from_numpy((keys % n).astype(np.int32))
+    assert len(cols) > 4 << 20
+    bias = torch.randn(len(cols), generator=torch.Generator().manual_seed(2))
+    heads, kv, c = 2, 1, 4
+    q, k, v, dy = att.operands(n, n, heads, kv, c, torch.float32)
+    A = att.build(indptr, cols, n, bias)
+    assert A.info()["symmetric_pattern"] == 1
+    att.check_all(att.run(A, q, k, v, dy, heads, kv, bias=True), att.reference(indptr, cols, q, k, v, dy, heads, kv, c ** -0.5, bias))
+
+
+def test_keys_and_values_beyond_4_gb():
+    """1.2 M rows of K and V, 4 KB each (4.9 GB an operand), of which the matrix reads the first, the last and some between."""
+    n, m, heads, c = 9, 1_200_000, 4, 256
+    gen = torch.Generator().manual_seed(0)
+    few = torch.cat([torch.arange(40), m // 2 + torch.arange(40), m - 40 + torch.arange(40)])
+    lengths = torch.tensor([0, 3, 700, 20, 1, 0, 90, 400, 2])
+    indptr = torch.zeros(n + 1, dtype=torch.int64)
+    indptr[1:] = lengths.cumsum(0)
+    pick = torch.randint(len(few), (int(indptr[-1]),), generator=gen)
+    r = lambda *s: torch.randn(*s, generator=gen)
+    q, dy, ks, vs = r(n, heads * c), r(n, heads * c), r(len(few), heads * c), r(len(few), heads * c)
+    k, v = (torch.empty(m, heads * c, device="cuda") for _ in range(2))
+    k[few.cuda()], v[few.cuda()] = ks.cuda(), vs.cuda()
+    A = att.build(indptr, few[pick].int(), m)
+    got = att.run(A, q.cuda(), k, v, dy.cuda(), heads, heads)
+    ref = att.reference(indptr, pick.int(), q, ks, vs, dy, heads, heads, c ** -0.5)
+    for name in ("dk", "dv"):
+        untouched = torch.ones(m, dtype=torch.bool, device="cuda")
+        untouched[few.cuda()] = False
+        assert not got[name].abs().amax(1)[untouched].any()
+        got[name] = got[name][few.cuda()]
+    att.check_all(got, ref)
+
+
+@pytest.mark.parametrize("dtype,pitch", [(torch.bfloat16, 1_500_000_001), (torch.float32, 1_100_000_003)], ids=["bfloat16", "float32"])
+def test_rows_far_apart(dtype, pitch):
+    """Rows whose offsets pass 2^32 bytes and 2^31 elements."""
+    n, d = 3, 700
+    def far(t):
+        full = torch.empty(2 * pitch + d, dtype=dtype, device="cuda")
+        out = torch.as_strided(full, (n, d), (pitch, 1))
+        if t is not None:
+            out.copy_(t)
+        return out
+    x, w, b, dy = norm.make(n, d, dtype, torch.float32)
+    got = norm.run(far(x), w, b, dy, dx=far(None))
+    ref = norm.reference(x, w, b, dy)
+    for name, t in got.items():
+        norm.check(t, ref, name)
+    z, labels, a, e = lab.make(n, d, dtype)
+    lab.check_all(lab.run(far(z), labels, 5, a, e, dz=far(None)), lab.reference(z, labels, 5, a, e))
+
+
+def test_slices_of_one_buffer():
+    """Queries, keys and values as column ranges of one projection's output, their gradients written into ranges of another."""
+    n, heads, c = 200, 4, 12
+    indptr, cols = att.graph(n, n, 5)
+    for dtype in (torch.float32, torch.bfloat16):
+        q, k, v, dy = att.operands(n, n, heads, heads, c, dtype)
+        w = heads * c
+        packed, grads = torch.cat([q, k, v], 1), torch.empty(n, 3 * w, dtype=dtype, device="cuda")
+        parts, outs = packed.split(w, 1), grads.split(w, 1)
+        A = att.build(indptr, cols, n)
+        got = att.run(A, *parts, dy, heads, heads, outs=(torch.empty_like(q), *outs))
+        att.check_all(got, att.reference(indptr, cols, q, k, v, dy, heads, heads, c ** -0.5))
+        g = ag.SparseGraph(indptr.cuda(), cols.cuda())
+        leaf = packed.clone().requires_grad_(True)
+        y = ag.attention(g, *leaf.split(w, 1), heads)
+        assert torch.equal(y, got["y"]) and torch.equal(torch.autograd.grad(y, leaf, dy)[0], grads)
+
+
+def test_norm_without_parameters_through_autograd():
+    x, w, b, dy = norm.make(50, 90, torch.float32, torch.float32)
+    one, zero = torch.ones_like(w), torch.zeros_like(b)
+    ref = norm.reference(x, one, zero, dy)
+    leaf = x.clone().requires_grad_(True)
+    norm.check(torch.autograd.grad(ag.layer_norm(leaf), leaf, dy)[0], ref, "dx")
+    bias = b.clone().requires_grad_(True)
+    y = ag.layer_norm(x, None, bias)
+    norm.check(torch.autograd.grad(y, bias, dy)[0], ref, "db")
+    half = norm.make(50, 90, torch.bfloat16, torch.bfloat16)
+    only = half[2].clone().requires_grad_(True)
+    got = torch.autograd.grad(ag.layer_norm(half[0], None, only), only, half[3])[0]
+    assert got.dtype == torch.bfloat16
+    norm.check(got, norm.reference(half[0], torch.ones(90), torch.zeros(90), half[3]), "db")
+
+
+def test_refusals_of_the_rowwise_calls():
+    x = torch.randn(6, 20, device="cuda")
+    w, f = torch.ones(20, device="cuda"), torch.empty(6, device="cuda")
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    labels = torch.zeros(6, dtype=torch.int64, device="cuda")
+    bad = [lambda: isp.layer_norm(x, y[:, 1:]), lambda: isp.layer_norm(x, y.half()), lambda: isp.layer_norm(x, y, w[1:]), lambda: isp.layer_norm(x, y, w.half()),
+           lambda: isp.layer_norm(x, y, w, torch.ones(40, device="cuda")[::2]), lambda: isp.layer_norm(x, y, w, mean=f[1:]), lambda: isp.layer_norm(x.double(), y.double()),
+           lambda: isp.layer_norm(x.t(), y.t()), lambda: isp.layer_norm(x[0], y[0]), lambda: isp.layer_norm(x, y, w, w.half()),
+           lambda: isp.layer_norm_backward(x, x, dx, None, f), lambda: isp.layer_norm_backward(x, x[1:], dx, f, f), lambda: isp.layer_norm_backward(x, x, dx[:, 1:], f, f),
+           lambda: isp.layer_norm_backward(x, x, dx, f, f, w, w.half()), lambda: isp.layer_norm_backward(x, x, dx, f, f, w, w, w, workspace=torch.empty(8, device="cuda")),
+           lambda: isp.label_logprob(x, labels[1:], f), lambda: isp.label_logprob(x, labels.int(), f), lambda: isp.label_logprob(x, labels, f.double()),
+           lambda: isp.label_logprob(x, labels, f, f[1:]), lambda: isp.label_logprob(x, labels, f, stats=f), lambda: isp.label_logprob(x, labels, f, top_logprob=torch.empty(6, 21, device="cuda")),
+           lambda: isp.label_logprob(x, labels, f, top_index=torch.empty(6, 2, device="cuda")), lambda: isp.label_logprob(x, labels, f, top_logprob=f),
+           lambda: isp.label_logprob_backward(x, labels, f, f, dx), lambda: isp.label_logprob_backward(x, labels, torch.empty(6, 2, device="cuda"), f, dx[:5]),
+           lambda: ag.label_logprob(x, labels, 21), lambda: ag.label_logprob(x, labels, -1), lambda: ag.label_logprob(x, labels.int()), lambda: ag.layer_norm(x, w[1:])]
+    for i, call in enumerate(bad):
+        with pytest.raises(AssertionError):
+            call()
+            print("call %d was taken" % i)
+    stats = torch.empty(6, 2, device="cuda")
+    for call in (lambda: isp.layer_norm(x, y, eps=-1.0), lambda: isp.layer_norm_backward(x, x, dx, f, f, w, w, w, workspace=torch.empty(16, dtype=torch.uint8, device="cuda")),
+                 lambda: isp.label_logprob(x, None, f), lambda: isp.label_logprob_backward(x, None, stats, f, dx), lambda: isp.label_logprob_backward(x, labels, stats, f, dx, d_entropy=f),
+                 lambda: isp.layer_norm(x[:, :0], y[:, :0])):
+        with pytest.raises(isp.IspError):
+            call()
+    wide = torch.randn(3, 100, device="cuda")
+    with pytest.raises(isp.IspError) as err:
+        isp.label_logprob(wide, labels[:3], f[:3], top_logprob=torch.empty(3, 65, device="cuda"))
+    assert err.value.status_name == "ISP_EUNSUPPORTED"
