@@ -308,8 +308,13 @@ isp_status isp_spmm_reduce(const isp_csr_t* A, const float* X, int64_t ldx, int3
 isp_status isp_spmm_reduce_backward(isp_csr_t* A, const float* dY, int64_t lddy, int32_t d, int reduce,
                                     const int32_t* arg, float* dX, int64_t lddx, void* stream);
 
-/* Bytes of device workspace isp_attention needs on A (0: none): the partial rows of the segments of split rows. */
-isp_status isp_attention_workspace(const isp_csr_t* A, int32_t heads, int32_t head_dim, size_t* bytes);
+/*
+ * Bytes of device workspace for isp_attention on A (0: none): the partial rows of the segments of split rows, and, where it pays (many entries
+ * per column, rows that are not whole lines), room for a copy of K and V side by side.  A workspace that only holds the former, (heads *
+ * (head_dim + 2)) floats per segment (isp_csr_info: n_segments) in whole 256 bytes, serves too: the call then reads K and V as they lie.
+ */
+isp_status isp_attention_workspace(const isp_csr_t* A, int32_t heads, int32_t kv_heads, int32_t head_dim, int dtype,
+                                   size_t* bytes);
 
 /*
  * Attention over the stored entries of A: FusedMM (Section 1(a)) with the softmax over each row's entries as its edge function, and
@@ -322,7 +327,8 @@ isp_status isp_attention_workspace(const isp_csr_t* A, int32_t heads, int32_t he
  *     any alignment that fits an element; dtype: ISP_F32 | ISP_BF16 | ISP_F16, of all four.  Scores, sums and products with P are held in 32 bits,
  *     Y is rounded once.  heads a multiple of kv_heads (at most 4096), head_dim <= 256.  Y must not overlap an operand.
  *   stats: fp32, n_rows x heads x 2, written for the backward: a reference m for the row's scores and the sum of exp(s - m).  May be NULL.
- *   workspace: 256-byte aligned, at least isp_attention_workspace bytes; used until the call's work on `stream` is done, nothing in it needs clearing.
+ *   workspace: 256-byte aligned, of isp_attention_workspace bytes; used until the call's work on `stream` is done, nothing in it needs clearing.
+ * Gathers are fastest from K and V that lie side by side in rows of whole 128-byte lines (column ranges of one projection's output).
  * Nothing of the handle's own scratch is used: calls on one handle may overlap, with a workspace each.
  */
 isp_status isp_attention(const isp_csr_t* A, const void* Q, int64_t ldq, const void* K, int64_t ldk, const void* V,

@@ -82,7 +82,7 @@ def load_library():
     lib.isp_spmm_reduce.argtypes = [vp, vp, i64, i32, ctypes.c_int, vp, i64, vp, vp]
     lib.isp_spmm_reduce_backward.argtypes = [vp, vp, i64, i32, ctypes.c_int, vp, vp, i64, vp]
     heads = [vp, vp, i64, vp, i64, vp, i64, i32, i32, i32, ctypes.c_float, u32, ctypes.c_int]
-    lib.isp_attention_workspace.argtypes = [vp, i32, i32, P(sz)]
+    lib.isp_attention_workspace.argtypes = [vp, i32, i32, i32, ctypes.c_int, P(sz)]
     lib.isp_attention.argtypes = heads + [vp, i64, vp, vp, sz, vp]
     lib.isp_attention_backward_workspace.argtypes = [vp, i32, i32, i32, P(sz)]
     lib.isp_attention_backward.argtypes = heads + [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, sz, vp]
@@ -475,11 +475,19 @@ def label_logprob_backward(Z, labels, stats, d_logprob, dZ, *, entropy=None, d_e
     return dZ
 
 
-def attention_workspace(A: CSR, heads: int, head_dim: int) -> int:
-    """isp_attention_workspace: bytes of device workspace a forward call on A needs."""
-    need = ctypes.c_size_t()
-    _check(load_library().isp_attention_workspace(A._h, int(heads), int(head_dim), ctypes.byref(need)))
-    return int(need.value)
+def _dtype_code(dtype) -> int:
+    import torch
+    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(dtype, -1)
+
+
+def attention_workspace(A: CSR, heads: int, head_dim: int, kv_heads=None, dtype=None) -> int:
+    """isp_attention_workspace: bytes of device workspace for a forward call on A (kv_heads: heads unless given; without a dtype enough for any).
+    A smaller workspace of the forward's partial rows alone serves too, see include/isp.h."""
+    need, most = ctypes.c_size_t(), 0
+    for code in (0, 1) if dtype is None else (_dtype_code(dtype),):
+        _check(load_library().isp_attention_workspace(A._h, int(heads), int(heads if kv_heads is None else kv_heads), int(head_dim), code, ctypes.byref(need)))
+        most = max(most, int(need.value))
+    return most
 
 
 def attention_backward_workspace(A: CSR, heads: int, kv_heads: int, head_dim: int) -> int:
@@ -501,8 +509,8 @@ def attention(A: CSR, Q, K, V, Y, heads: int, kv_heads=None, *, scale=None, bias
     heads = int(heads)
     kv_heads = heads if kv_heads is None else int(kv_heads)
     c = _head_dim(Q, heads)
-    if workspace is None and c:
-        workspace = _call_workspace(None, attention_workspace(A, heads, c), Q, stream)
+    if workspace is None and c and kv_heads > 0 and heads % kv_heads == 0 and _dtype_code(Q.dtype) >= 0:
+        workspace = _call_workspace(None, attention_workspace(A, heads, c, kv_heads, Q.dtype), Q, stream)
     st = _nat.attention(A._cell, Q, K, V, Y, stats, workspace, heads, kv_heads, float(scale if scale is not None else max(c, 1) ** -0.5),
                         ISP_BIAS_BY_A if bias else 0, _raw(stream))
     if st:

@@ -705,6 +705,27 @@ __global__ void __launch_bounds__(ISP_WG) k_att_col_fixup(isp_view A, att_args a
   else att_out(a, a.carry2, static_cast<T*>(a.y2), (int64_t)row * half + col - half, (int64_t)row * a.ldy2 + col - half, y);
 }
 
+// K's and V's rows next to each other in rows of whole lines: 16 bytes a thread.
+template <class T>
+__global__ void __launch_bounds__(ISP_WG) k_att_pack(att_args a, uint32_t pitch) {
+  constexpr int W = 16 / sizeof(T);
+  const uint32_t per_row = pitch / 16;
+  const int width = a.kv_heads * a.dh;
+  const int64_t total = a.n_cols * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * ISP_WG + threadIdx.x; i < total; i += (int64_t)gridDim.x * ISP_WG) {
+    const int64_t row = i / per_row;
+    const int e = (int)(i - row * per_row) * W;
+    const T *k = att_row<T>(a.k, (uint32_t)row, a.pk), *v = att_row<T>(a.v, (uint32_t)row, a.pv);
+    raw_t<T, W> o;
+    if (e + W <= width) o = load_raw<T, W>(k + e);
+    else if (e >= width && e + W <= 2 * width) o = load_raw<T, W>(v + (e - width));
+    else
+#pragma unroll
+      for (int j = 0; j < W; ++j) o[j] = e + j < width ? k[e + j] : e + j < 2 * width ? v[e + j - width] : (T)0.f;
+    *reinterpret_cast<raw_t<T, W>*>(static_cast<char*>(a.packed) + row * pitch + (int64_t)e * sizeof(T)) = o;
+  }
+}
+
 // ---- host ------------------------------------------------------------------------------------------------------------
 // chunks: of a key head's query heads, side by side (blockIdx.z)
 template <class P, int LPG>
@@ -746,6 +767,16 @@ template <class T>
 isp_status att_forward(const isp_csr* A, att_args a, hipStream_t s) {
   const isp_view& v = A->v;
   const int rq = att_share(a.group, 4);
+  if (a.packed) {
+    const int64_t row_bytes = (int64_t)a.kv_heads * a.dh * sizeof(T);
+    const uint32_t pitch = (uint32_t)att_packed_pitch(row_bytes);
+    const int64_t groups = (a.n_cols * (pitch / 16) + ISP_WG - 1) / ISP_WG;
+    k_att_pack<T><<<(unsigned)(groups < 65536 ? groups : 65536), ISP_WG, 0, s>>>(a, pitch);
+    ISP_LAUNCH_CHECK();
+    a.k = a.packed;
+    a.v = static_cast<const char*>(a.packed) + row_bytes;
+    a.pk = a.pv = pitch;
+  }
   isp_status st = att_pass<att_fwd, T>(v, a, rq, a.group / rq,
                                      att_wide(sizeof(T), a.group, a.kv_heads, a.dh, A->info.nnz, A->info.n_rows - A->info.bin_rows[0]), s);
   if (st != ISP_OK || v.n_hub == 0) return st;

@@ -42,6 +42,11 @@ isp_status check_workspace(const void* ws, size_t have, size_t need) {
 }
 
 size_t forward_bytes(const isp_csr* A, int32_t heads, int32_t dh) { return isp_align((size_t)A->v.n_seg * heads * (dh + 2) * sizeof(float)); }
+// and for the copy of K and V, where the rule takes one
+size_t packed_bytes(const isp_csr* A, int32_t kv_heads, int32_t dh, int dtype, bool whole) {
+  const int64_t row = (int64_t)kv_heads * dh * (dtype == ISP_F32 ? 4 : 2);
+  return isp_dev::att_packs(row, whole, A->v.nnz, A->v.n_cols) ? (size_t)A->v.n_cols * isp_dev::att_packed_pitch(row) : 0;
+}
 
 struct backward_space {  // (offsets)
   size_t part, carry, carry2, total;
@@ -74,10 +79,12 @@ att_args make_args(int32_t heads, int32_t kv_heads, int32_t dh, float scale, uns
 
 extern "C" {
 
-isp_status isp_attention_workspace(const isp_csr_t* A, int32_t heads, int32_t head_dim, size_t* bytes) {
+isp_status isp_attention_workspace(const isp_csr_t* A, int32_t heads, int32_t kv_heads, int32_t head_dim, int dtype, size_t* bytes) {
   if (!bytes) return isp_fail(ISP_EINVAL, "bytes is NULL");
-  ISP_TRY(check_heads(A, heads, heads, head_dim));
-  *bytes = forward_bytes(A, heads, head_dim);
+  ISP_TRY(check_heads(A, heads, kv_heads, head_dim));
+  ISP_TRY(check_type(dtype, 0, A));
+  const int64_t row = (int64_t)kv_heads * head_dim * (dtype == ISP_F32 ? 4 : 2);  // (dense rows)
+  *bytes = forward_bytes(A, heads, head_dim) + packed_bytes(A, kv_heads, head_dim, dtype, row % isp_dev::ATT_LINE == 0);
   return ISP_OK;
 }
 
@@ -100,6 +107,12 @@ isp_status isp_attention(const isp_csr_t* A, const void* Q, int64_t ldq, const v
   a.y = Y, a.ldy = ldy;
   a.stats = stats;
   a.part = static_cast<float*>(workspace);
+  const auto lines = [&](const void* p, int64_t ld) { return (uintptr_t)p % isp_dev::ATT_LINE == 0 && ld * size % isp_dev::ATT_LINE == 0; };
+  const size_t copy = packed_bytes(A, kv_heads, head_dim, dtype, lines(K, ldk) && ldv == ldk && (uintptr_t)V % 4 == 0);
+  if (copy && workspace_bytes >= forward_bytes(A, heads, head_dim) + copy) {
+    a.packed = static_cast<char*>(workspace) + forward_bytes(A, heads, head_dim);
+    a.n_cols = A->v.n_cols;
+  }
   if (dtype == ISP_F32) return isp_att_forward_f32(A, a, (hipStream_t)stream);
   if (dtype == ISP_BF16) return isp_att_forward_bf16(A, a, (hipStream_t)stream);
   return isp_att_forward_f16(A, a, (hipStream_t)stream);

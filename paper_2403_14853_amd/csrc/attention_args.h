@@ -21,6 +21,8 @@ struct att_args {
   int bias;                  // the matrix's values are added to the scores
   void *y, *y2;              // output rows (forward y, backward dq or dk; y2: dv)
   int64_t ldy, ldy2;         // in elements
+  void* packed;              // forward: room for K's and V's rows next to each other (NULL: they are read as they lie)
+  int64_t n_cols;
   float* stats;              // (m, l) per row and head: written by the forward (may be NULL), read by the backward
   att_num* stat;             // backward, per row and head, in the workspace
   float* part;               // partial rows of the split rows' segments, in the workspace

@@ -27,4 +27,19 @@ inline bool att_wide(int element_bytes, int group, int kv_heads, int dh, int64_t
   return element_bytes == 2 && group == 1 && dh >= 8 && att_lanes_per_head(dh, 8) * kv_heads >= 5 && nnz >= 16 * live_rows;
 }
 
+// The forward copies K and V next to each other into rows of whole lines (pitch: att_packed_pitch) where that saves its gathers more than it costs.
+// A row of x bytes lies on ceil(x / 128) lines where rows start on lines, else on x / 128 + 1 on average; the copy moves its bytes at 4.5 TB/s, and its launch is 4 us.
+// A line less per entry saves 1 ps where the launch is bound by the vector ALU or L2 has the rows, up to 6 where gathers miss; the rule takes 1.5.  us with K and V as they
+// lie / side by side, and the copy: 233 k columns, 40 M entries: 3 heads of 20, 16-bit 987 / 910, 30; 1 of 16 452 / 356, 14; 200 k, 10 M: 4 of 7, fp32 257 / 162, 25; uniform, 100 k, 6 M: 1 of
+// 32, 16-bit 149 / 83, 10; 60 k, 6 M: 1 of 50, 16-bit 125 / 105, 10; not taken: 1 M, 17 M: 2 key heads of 16, 16-bit 640 / 629, 64, and 1 of 32 337 / 241, 64; 169 k, 2.4 M: 3 of 20, 16-bit 95 / 82, 23, and 2 of
+// 50, fp32 237 / 204, 68; 60 k, 6 M: 3 of 33, fp32 434 / 434, 27.
+constexpr int ATT_LINE = 128;
+inline int64_t att_packed_pitch(int64_t row_bytes) { return (2 * row_bytes + ATT_LINE - 1) / ATT_LINE * ATT_LINE; }
+// whole: rows of K and V start on lines
+inline bool att_packs(int64_t row_bytes, bool whole, int64_t nnz, int64_t n_cols) {
+  const double lines = whole ? (double)((row_bytes + ATT_LINE - 1) / ATT_LINE) : (double)row_bytes / ATT_LINE + 1.;
+  const double saved = 2. * lines - (double)(att_packed_pitch(row_bytes) / ATT_LINE);
+  return 1.5e-6 * saved * (double)nnz > 4. + (double)n_cols * (double)(2 * row_bytes + att_packed_pitch(row_bytes)) / 4.5e6;
+}
+
 }  // namespace isp_dev

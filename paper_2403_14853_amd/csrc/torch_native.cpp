@@ -1145,7 +1145,7 @@ PyObject* py_ag_attention(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
       const Mat O = mat(Y);
       if (grad) stats = floats_like(q, {MQ.rows, heads, 2});
       size_t bytes = 0;
-      check(isp_attention_workspace(g->A->h.load(), H.heads, H.dim, &bytes));
+      check(isp_attention_workspace(g->A->h.load(), H.heads, H.kv, H.dim, MQ.type, &bytes));
       Tensor ws;
       if (bytes) ws = workspace_like(q, bytes);
       sync_values(*g);

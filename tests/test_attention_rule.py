@@ -23,6 +23,14 @@ int main() {
   CHECK(att_wide(2, 1, 8, 8, 1600, 100) && !att_wide(2, 1, 8, 8, 1599, 100) && !att_wide(4, 1, 8, 8, 1600, 100) && !att_wide(2, 2, 8, 8, 1600, 100));
   CHECK(!att_wide(2, 1, 8, 7, 1600, 100) && !att_wide(2, 1, 4, 8, 1600, 100) && !att_wide(2, 1, 2, 16, 1600, 100) && att_wide(2, 1, 3, 20, 1600, 100));
   CHECK(att_wide(2, 1, 1, 64, 1600, 100) && !att_wide(2, 1, 1, 32, 1600, 100));
+  for (int64_t x = 2; x <= 4096; x += 2) {
+    const int64_t p = att_packed_pitch(x);
+    CHECK(p % 128 == 0 && p >= 2 * x && p < 2 * x + 128);
+    CHECK(!att_packs(x, false, 0, 1000) && !att_packs(x, false, 1000, 1000) && !att_packs(x, true, 4 * 1000 * 1000, 1000 * 1000));
+    if (x % 128 == 0) CHECK(!att_packs(x, true, int64_t(1) << 31, 1000));  // (nothing is saved)
+  }
+  CHECK(att_packs(120, false, 40000003, 232965) && !att_packs(120, false, 2404585, 169343) && !att_packs(64, true, 16851165, 1048576));
+  CHECK(att_packs(100, false, 6000000, 60000) && att_packs(64, true, 16851165, 300000));
   return 0;
 }
 """

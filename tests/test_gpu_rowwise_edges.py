@@ -61,6 +61,29 @@ def test_shared_transpose_of_a_large_symmetric_pattern():
     att.check_all(att.run(A, q, k, v, dy, heads, kv, bias=True), att.reference(indptr, cols, q, k, v, dy, heads, kv, c ** -0.5, bias))
 
 
+@pytest.mark.parametrize("heads,kv,c,dtype", [(3, 3, 20, torch.float16), (1, 1, 7, torch.bfloat16), (2, 1, 50, torch.float32), (4, 2, 3, torch.float32)])
+def test_copy_of_keys_and_values(heads, kv, c, dtype):
+    """Many entries per column: K and V are copied side by side where the workspace has room, with the same bits as without."""
+    n, m = 8000, 600
+    gen = np.random.default_rng(c)
+    lengths = gen.integers(0, 700, n)
+    indptr = torch.zeros(n + 1, dtype=torch.int64)
+    indptr[1:] = torch.from_numpy(lengths).cumsum(0)
+    cols = torch.from_numpy(gen.integers(0, m, int(indptr[-1])).astype(np.int32))
+    q, k, v, dy = att.operands(n, m, heads, kv, c, dtype, gap=1, offset=1)
+    A = isp.csr_build(indptr.cuda(), cols.cuda(), None, n_cols=m)
+    full = isp.attention_workspace(A, heads, c, kv, dtype)
+    least = (A.info()["n_segments"] * heads * (c + 2) * 4 + 255) // 256 * 256
+    row = kv * c * (4 if dtype == torch.float32 else 2)
+    assert full - least == m * ((2 * row + 127) // 128 * 128) and isp.attention_workspace(A, heads, c) >= full
+    results = []
+    for size in (full, least, full - 1):
+        ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+        results.append(isp.attention(A, q, k, v, torch.empty_like(q), heads, kv, workspace=ws))
+    assert torch.equal(results[0], results[1]) and torch.equal(results[0], results[2])
+    att.check(results[0], att.reference(indptr, cols, q, k, v, dy, heads, kv, c ** -0.5), "y")
+
+
 def test_keys_and_values_beyond_4_gb():
     """1.2 M rows of K and V, 4 KB each (4.9 GB an operand), of which the matrix reads the first, the last and some between."""
     n, m, heads, c = 9, 1_200_000, 4, 256

@@ -60,7 +60,7 @@ def test_label_logprob_at_the_c_boundary(lib):
 
 def test_attention_at_the_c_boundary(lib):
     need = ctypes.c_size_t()
-    assert lib.isp_attention_workspace(None, 2, 8, ctypes.byref(need)) == EINVAL and lib.isp_attention_workspace(None, 2, 8, None) == EINVAL
+    assert lib.isp_attention_workspace(None, 2, 2, 8, 0, ctypes.byref(need)) == EINVAL and lib.isp_attention_workspace(None, 2, 2, 8, 0, None) == EINVAL
     assert lib.isp_attention_backward_workspace(None, 2, 2, 8, ctypes.byref(need)) == EINVAL
     assert lib.isp_attention(None, P, 16, P, 16, P, 16, 2, 2, 8, 1.0, 0, 0, P, 16, None, None, 0, None) == EINVAL
     assert lib.isp_attention_backward(None, P, 16, P, 16, P, 16, 2, 2, 8, 1.0, 0, 0, P, P, 16, P, 16, P, 16, P, 16, None, 0, None) == EINVAL
