@@ -123,7 +123,7 @@ __device__ __forceinline__ const T* att_row(const void* base, uint32_t row, uint
 template <class T_, int W_, int RQ_, bool TINY_>
 struct att_fwd {
   using T = T_;
-  static constexpr int W = W_, RQ = RQ_, RING = 4, PARTS = RQ, MOST = 4, WAVES = 1;
+  static constexpr int W = W_, RQ = RQ_, RING = 4, PARTS = RQ, MOST = 4;
   static constexpr bool WIDE = true;
   static constexpr bool TINY = TINY_;
   using lane_t = att_lane<W, TINY>;
@@ -257,7 +257,7 @@ __device__ __forceinline__ float att_weight(float z, const att_num& st) { return
 template <class T_, int W_, int RQ_, bool TINY_>
 struct att_bwd_row {
   using T = T_;
-  static constexpr int W = W_, RQ = RQ_, RING = 4, PARTS = RQ, MOST = 2, WAVES = 1;
+  static constexpr int W = W_, RQ = RQ_, RING = 4, PARTS = RQ, MOST = 2;
   static constexpr bool WIDE = false;
   static constexpr bool TINY = TINY_;
   using lane_t = att_lane<W, TINY>;
@@ -383,7 +383,7 @@ __device__ __forceinline__ void att_out(const att_args& a, float* carry, T* out,
 template <class T_, int W_, int RQ_, bool TINY_>
 struct att_bwd_col {
   using T = T_;
-  static constexpr int W = W_, RQ = RQ_, RING = RQ == 1 ? 4 : 2, PARTS = 1, MOST = 4, WAVES = RQ == 4 ? 3 : 1;
+  static constexpr int W = W_, RQ = RQ_, RING = RQ == 1 ? 4 : 2, PARTS = 1, MOST = 4;
   static constexpr bool WIDE = false;
   static constexpr bool TINY = TINY_;
   using lane_t = att_lane<W, TINY>;
@@ -503,7 +503,7 @@ struct att_bwd_col {
 
 // ---- a pass ----------------------------------------------------------------------------------------------------------
 template <class P, int LPG>
-__global__ void __launch_bounds__(ISP_WG, P::WAVES) k_att(isp_view A, const int64_t* __restrict__ indptr, const int32_t* __restrict__ indices,
+__global__ void __launch_bounds__(ISP_WG) k_att(isp_view A, const int64_t* __restrict__ indptr, const int32_t* __restrict__ indices,
                                                 const float* __restrict__ bias, att_args a) {
   __shared__ rn_lds lds;
   constexpr int G = ISP_WAVE / LPG, RING = P::RING, CHUNK = RING % 4 == 0 ? 2 : 1;
