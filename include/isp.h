@@ -8,6 +8,8 @@
  *   SDDMM  one dot product per stored entry of A (gives dA of SpMM)       (Section 1)
  *   FusedMM SDDMM -> edge function -> SpMM in one pass, edge matrix never
  *          written; sigmoid instance, forward and backward               (Section 1(a))
+ *   attention over A's entries (FusedMM with a row's softmax), layer norm and the log probabilities of labels: the training step's
+ *          operators around the sparse products, forward and backward, fp32 / bf16 / fp16
  *
  * General conventions
  *   - Every array pointer is a DEVICE pointer on the current HIP device unless its name starts
@@ -17,7 +19,7 @@
  *   - CSR: indptr int64[n_rows+1], indices int32[nnz], values fp32[nnz] or NULL (all ones).
  *     Columns inside a row may be unsorted and may repeat; a repeated column is a separate
  *     stored entry (SpMM adds them, SDDMM emits one output per stored entry).
- *   - Dense matrices are fp32 row-major; ld* is the distance between rows in elements (>= d).  Any ld and
+ *   - Dense matrices are row-major, fp32 unless an operator takes an element type; ld* is the distance between rows in elements (>= d).  Any ld and
  *     alignment is accepted; rows that start on 128-byte lines (ld a multiple of 32, base pointer aligned)
  *     gather fastest.
  *   - stream is a hipStream_t passed as void* (NULL = the default stream).  Compute calls are
