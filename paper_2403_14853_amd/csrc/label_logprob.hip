@@ -480,6 +480,7 @@ __global__ void __launch_bounds__(ISP_WG) k_lp_chunk_bwd(lp_bwd_args g) {
 
 // ---- host ------------------------------------------------------------------------------------------------------------
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int64_t LP_THREADS = 1ll << 31;  // of a launch, which has to stay below 2^32 of them
 
 // A wavefront per row where there are rows for all of the chip's wavefronts, or a workgroup would have less than a tile for each of its own.
 bool lp_wave_rows(int64_t n, int classes) { return n >= 4096 || classes <= 2 * LP_TILE; }
@@ -527,9 +528,21 @@ void lp_run(const lp_args& a, hipStream_t s) {
   if (a.classes <= LP_GROUP) return lp_short_rows<T>(a, s);
   const int bt = LP_WAVES * ISP_WAVE;
   if (lp_wave_rows(a.n, a.classes)) {
-    const unsigned grid = (unsigned)ceil_div(a.n, LP_WAVES);
-    if (a.top > 0) k_lp_stream<T, 1, true><<<grid, bt, 0, s>>>(a);
-    else k_lp_stream<T, 1, false><<<grid, bt, 0, s>>>(a);
+    constexpr int64_t MOST = LP_THREADS / ISP_WAVE;
+    for (int64_t r0 = 0; r0 < a.n; r0 += MOST) {
+      lp_args b = a;
+      b.z = static_cast<const T*>(a.z) + r0 * a.ldz;
+      b.n = a.n - r0 < MOST ? a.n - r0 : MOST;
+      if (a.labels) b.labels += r0;
+      if (a.logprob) b.logprob += r0;
+      if (a.entropy) b.entropy += r0;
+      if (a.stats) b.stats += 2 * r0;
+      if (a.top_logprob) b.top_logprob += r0 * a.top;
+      if (a.top_index) b.top_index += r0 * a.top;
+      const unsigned grid = (unsigned)ceil_div(b.n, LP_WAVES);
+      if (a.top > 0) k_lp_stream<T, 1, true><<<grid, bt, 0, s>>>(b);
+      else k_lp_stream<T, 1, false><<<grid, bt, 0, s>>>(b);
+    }
     return;
   }
   const unsigned grid = (unsigned)(a.n * a.splits);
@@ -544,7 +557,7 @@ template <class T>
 void lp_run(const lp_bwd_args& a, hipStream_t s) {
   if (a.classes <= LP_GROUP) return lp_short_rows<T>(a, s);
   const int64_t total = a.n * a.chunks;
-  k_lp_chunk_bwd<T><<<(unsigned)(total < (1 << 30) ? total : 1 << 30), ISP_WG, 0, s>>>(a);
+  k_lp_chunk_bwd<T><<<(unsigned)(total < LP_THREADS / ISP_WG ? total : LP_THREADS / ISP_WG), ISP_WG, 0, s>>>(a);
 }
 
 }  // namespace

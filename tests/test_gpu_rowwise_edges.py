@@ -190,3 +190,47 @@ def test_refusals_of_the_rowwise_calls():
     with pytest.raises(isp.IspError) as err:
         isp.label_logprob(wide, labels[:3], f[:3], top_logprob=torch.empty(3, 65, device="cuda"))
     assert err.value.status_name == "ISP_EUNSUPPORTED"
+
+
+def test_more_long_rows_than_a_launch_has_threads_for():
+    """Rows of 1030 scores, more than 2^25 of them, whose backward has more than 2^24 workgroups' chunks: 2 x 70 GB in bf16."""
+    n, c = (1 << 25) + 13, 1030
+    if torch.cuda.mem_get_info()[0] < 150e9:
+        pytest.skip("needs 150 GB of device memory")
+    z = torch.zeros(n, c, dtype=torch.bfloat16, device="cuda")
+    picks = torch.tensor([0, 1, 7, 8, (1 << 24) - 1, 1 << 24, (1 << 25) - 1, 1 << 25, (1 << 25) + 1, n - 1], device="cuda")
+    gen = torch.Generator().manual_seed(0)
+    rows = torch.randn(len(picks), c, generator=gen).bfloat16()
+    z[picks] = rows.cuda()
+    labels = torch.arange(n, device="cuda") % c
+    lp, en, stats = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty(n, 2, device="cuda")
+    tv, ti = torch.empty(n, 2, device="cuda"), torch.empty(n, 2, dtype=torch.int32, device="cuda")
+    isp.label_logprob(z, labels, lp, en, stats=stats, top_logprob=tv, top_index=ti)
+    p = rows.double().log_softmax(1)
+    at = labels[picks].cpu()
+    # (two roundings of the maximum's difference and the logarithm, and a sum of 1030 terms in 32 bits: under 2^-18 of numbers below 16)
+    tol = 16 * 2.0 ** -18
+    assert (lp[picks].cpu().double() - p[torch.arange(len(picks)), at]).abs().max() < tol
+    assert (en[picks].cpu().double() + (p.exp() * p).sum(1)).abs().max() < tol
+    assert (tv[picks].cpu().double() - p.topk(2).values).abs().max() < tol
+    other = torch.ones(n, dtype=torch.bool, device="cuda")
+    other[picks] = False
+    log_c = float(np.log(c))
+    assert (lp + log_c)[other].abs().max() < tol and (en - log_c)[other].abs().max() < tol and (tv + log_c)[other].abs().max() < tol
+    assert torch.equal(ti[other], torch.tensor([[0, 1]], dtype=torch.int32, device="cuda").expand(n - len(picks), 2))
+    del tv, ti, other
+    dz = torch.full_like(z, 7.0)
+    isp.label_logprob_backward(z, labels, stats, torch.ones(n, device="cuda"), dz)
+    want = torch.nn.functional.one_hot(at, c).double() - p.exp()
+    assert ((dz[picks].cpu().double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -15).all()
+    # every other row: 1 - 1/c at its label, -1/c elsewhere, rounded to bf16
+    there, elsewhere = (torch.tensor(x).bfloat16().item() for x in (1 - 1 / c, -1 / c))
+    for r0 in range(0, n, 1 << 22):
+        part = dz[r0:r0 + (1 << 22)]
+        skip = picks[(picks >= r0) & (picks < r0 + (1 << 22))] - r0
+        got = part.gather(1, labels[r0:r0 + (1 << 22), None])[:, 0]
+        got[skip] = there
+        assert (got == there).all()
+        part.scatter_(1, labels[r0:r0 + (1 << 22), None], elsewhere)
+        part[skip] = elsewhere
+        assert part.min().item() == elsewhere and part.max().item() == elsewhere
