@@ -438,8 +438,8 @@ def layer_norm_backward_workspace(n: int, d: int) -> int:
 
 def layer_norm_backward(X, dY, dX, mean, rstd, weight=None, dweight=None, dbias=None, *, workspace=None, stream=None):
     """isp_layer_norm_backward; dX, dweight, dbias: None where not wanted.  Returns dX."""
-    if (dweight is not None or dbias is not None) and X.dim() == 2 and X.shape[1] > 0:
-        workspace = _call_workspace(workspace, layer_norm_backward_workspace(*X.shape), X, stream)
+    if workspace is None and (dweight is not None or dbias is not None) and X.dim() == 2 and X.shape[1] > 0:
+        workspace = _call_workspace(None, layer_norm_backward_workspace(*X.shape), X, stream)
     st = _native().layer_norm_backward(X, dY, dX, mean, rstd, weight, dweight, dbias, workspace, _raw(stream))
     if st:
         _check(st)
