@@ -324,8 +324,8 @@ isp_status isp_attention_workspace(const isp_csr_t* A, int32_t heads, int32_t kv
  *   s_p = scale <Q[i, h], K[j, g]> (+ values[p] with ISP_BIAS_BY_A),   P = softmax of s over the row's entries,   Y[i, h] = sum_p P_p V[j, g].
  * A says which keys a query sees: a graph, a batch of graphs of different sizes (block diagonal), a causal or any other pattern.  Repeated columns
  * are entries of their own.  Without ISP_BIAS_BY_A the values are not looked at.  A bias of -inf masks its entry, whatever K and V hold there.
- * Rows without entries, or with masked ones only: Y = 0.  Of other entries a score of -inf has no weight, one of +inf or NaN makes its row and head
- * NaN, an infinity or NaN in V the column that it stands in infinite or NaN.
+ * Rows without entries, or with masked ones only: Y = 0.  An infinity or NaN in the operands of an entry that is not masked stays in its row and
+ * head: one in Q or K may make them NaN (a score of +inf or NaN does), one in V makes its column infinite or NaN.
  *   Q, Y: n_rows x (heads * head_dim), K, V: n_cols x (kv_heads * head_dim), row-major, head after head; any ld (rows less than 4 GB apart) and
  *     any alignment that fits an element; dtype: ISP_F32 | ISP_BF16 | ISP_F16, of all four.  Scores, sums and products with P are held in 32 bits,
  *     Y is rounded once.  heads a multiple of kv_heads (at most 4096), head_dim <= 256.  Y must not overlap an operand.

@@ -234,3 +234,41 @@ def test_more_long_rows_than_a_launch_has_threads_for():
         part.scatter_(1, labels[r0:r0 + (1 << 22), None], elsewhere)
         part[skip] = elsewhere
         assert part.min().item() == elsewhere and part.max().item() == elsewhere
+
+
+@pytest.mark.parametrize("heads,kv,c,dtype", [(4, 2, 12, torch.float32), (1, 1, 64, torch.bfloat16), (3, 3, 5, torch.float16), (8, 1, 3, torch.float32)])
+def test_infinite_scores_and_values(heads, kv, c, dtype):
+    """Columns of K that make scores of +inf and NaN, columns of V with an infinity and a NaN, in short rows and in split ones."""
+    n, m = 300, 200
+    gen = torch.Generator().manual_seed(3)
+    lengths = torch.randint(1, 6, (n,), generator=gen)
+    lengths[[5, 50, 150, 222]] = 3000
+    indptr = torch.zeros(n + 1, dtype=torch.int64)
+    indptr[1:] = lengths.cumsum(0)
+    cols = torch.randint(10, m, (int(indptr[-1]),), generator=gen).int()
+    r = lambda rows, heads: torch.randn(rows, heads * c, generator=gen).to(dtype).cuda()
+    q, k, v = r(n, heads), r(m, kv), r(m, kv)
+    q[:, ::c] = q[:, ::c].abs() + 0.5  # (the first column of each head: the sign of what K holds there is the score's)
+    highest, none, inf_v, nan_v = range(4)
+    seen = ({30, 5}, {40, 50}, {60, 150, 222}, {70, 222})
+    for col in range(4):
+        for row in seen[col]:
+            cols[indptr[row] + (0 if row % 10 == 0 and lengths[row] < 10 else 800 + 700 * col)] = col
+    k[highest, ::c], k[none, ::c] = np.inf, np.nan
+    v[inf_v, 0::c], v[nan_v, 1::c] = np.inf, np.nan
+    y = isp.attention(att.build(indptr, cols, m), q, k, v, torch.empty_like(q), heads, kv)
+    kc, vc = k.clone(), v.clone()
+    kc[:10], vc[:10] = 0, 0
+    value, bound = att.reference(indptr, cols, q, kc, vc, q, heads, kv, c ** -0.5)["y"]
+    room = bound + att.half_step(value, dtype) * 1.001 + 1e-37
+    y = y.double().cpu().view(n, heads, c)
+    right = ((y - value.view(n, heads, c)).abs() <= room.view(n, heads, c)).flatten(1).all(1)
+    for row in range(n):
+        if row in seen[highest] | seen[none]:
+            assert torch.isnan(y[row]).all(), row
+        elif row in seen[inf_v] | seen[nan_v]:
+            bad = torch.zeros(c, dtype=torch.bool)
+            bad[0], bad[1] = row in seen[inf_v], row in seen[nan_v]
+            assert not torch.isfinite(y[row][:, bad]).any() and torch.isfinite(y[row][:, ~bad]).all(), row
+        else:
+            assert right[row], row
