@@ -272,3 +272,36 @@ def test_infinite_scores_and_values(heads, kv, c, dtype):
             assert not torch.isfinite(y[row][:, bad]).any() and torch.isfinite(y[row][:, ~bad]).all(), row
         else:
             assert right[row], row
+
+
+def test_attention_on_an_alias():
+    """A second handle on the matrix, with its own copy of the cached transpose: the same bits, also beside calls on the first one; refused once stale."""
+    n, m, heads, kv, c = 400, 300, 4, 2, 20
+    indptr, cols = att.graph(n, m, 9)
+    bias = torch.randn(len(cols), generator=torch.Generator().manual_seed(1))
+    A = att.build(indptr, cols, m, bias)
+    B = isp.csr_alias(A)
+    q, k, v, dy = att.operands(n, m, heads, kv, c, torch.bfloat16)
+    want = att.run(A, q, k, v, dy, heads, kv, bias=True)
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        got = att.run(B, q, k, v, dy, heads, kv, bias=True)
+    again = att.run(A, q, k, v, dy, heads, kv, bias=True)
+    torch.cuda.synchronize()
+    for name in want:
+        assert torch.equal(got[name], want[name]) and torch.equal(again[name], want[name]), name
+    att.check_all(want, att.reference(indptr, cols, q, k, v, dy, heads, kv, c ** -0.5, bias))
+    isp.csr_values_changed(A)
+    with pytest.raises(isp.IspError):
+        isp.attention(B, q, k, v, torch.empty_like(q), heads, kv)
+
+
+@pytest.mark.parametrize("heads,kv,c,dtype", [(4096, 4096, 2, torch.float32), (4096, 512, 3, torch.bfloat16), (192, 3, 4, torch.float16), (64, 1, 256, torch.float32)])
+def test_many_heads(heads, kv, c, dtype):
+    n, m = 12, 9
+    indptr, cols = att.graph(n, m, 2, hubs=((3, 1300),), longest=5)
+    q, k, v, dy = att.operands(n, m, heads, kv, c, dtype)
+    att.check_all(att.run(att.build(indptr, cols, m), q, k, v, dy, heads, kv), att.reference(indptr, cols, q, k, v, dy, heads, kv, c ** -0.5))
+    with pytest.raises(isp.IspError):
+        isp.attention(att.build(indptr, cols, m), *(torch.zeros(r, 4097 * 2, device="cuda") for r in (n, m, m, n)), 4097)
