@@ -1,7 +1,7 @@
 // Attention over the stored entries of a CSR matrix (gfx950, wave64): the three passes' kernels, instantiated per element type in attention_*.hip.
 //   forward   s_p = scale <q_i, k_j> + bias_p,  P = softmax over row i's entries,  y_i = sum_p P_p v_j           (p = (i, j))
 //   backward  t_p = <dy_i, v_j>,  D_i = sum_p P_p t_p,  dS_p = P_p (t_p - D_i)
-//             rows of A:    dq_i = scale sum_p dS_p k_j = scale (sum_p P_p t_p k_j - D_i sum_p P_p k_j)
+//             rows of A:    dq_i = scale sum_p dS_p k_j = scale / l_i (sum_p e_p t_p k_j - D_i sum_p e_p k_j),  e_p = exp(s_p - m_i) = P_p l_i
 //             rows of A^T:  dk_j = scale sum_p dS_p q_i,   dv_j = sum_p P_p dy_i
 // with `heads` query heads on `kv_heads` key heads: query head h reads key head h / R, R = heads / kv_heads.
 //
@@ -29,14 +29,37 @@ constexpr float ATT_SLACK = 8.f;
 // The reference of a row that has met nothing: finite, so that differences to it are numbers; a score of -inf is below it, too.
 constexpr float ATT_NONE = -3.402823466e38f;
 
+// What a lane leaves in of its vector of a row operand: its own elements, as factors (fp32), or as bits that products of 16-bit pairs take (att_dot).
+template <class T, int W>
+struct att_mask {
+  typedef uint32_t bits __attribute__((ext_vector_type(W / 2)));
+  bits keep;
+  __device__ __forceinline__ void set(int j, bool own, float) {
+    const uint32_t half = 0xffffu << (16 * (j & 1));
+    keep[j / 2] = (j & 1 ? keep[j / 2] : 0u) | (own ? half : 0u);
+  }
+};
+template <int W>
+struct att_mask<float, W> {
+  float own[W], scaled[W];  // 1 or the scale for those, else 0
+  __device__ __forceinline__ void set(int j, bool o, float scale) {
+    own[j] = o ? 1.f : 0.f;
+    scaled[j] = o ? scale : 0.f;
+  }
+};
+// Whether the values are added to the scores, as an entry's work asks or knows.  The loops with eight columns to a lane, which serve long rows, are there
+// with and without: a step without branches is one block to the compiler (233 k rows, 40 M entries, 3 heads of 20, fp16 935 / 864 us).  With four
+// the kernels would double for nothing (forward, 1 M rows, 17 M entries 660 / 669, rows 1111 / 1156).
+constexpr int ATT_PLAIN = 0, ATT_BIAS = 1, ATT_ASK = 2;
+
 // Where a lane works.
-template <int W, bool TINY>
+template <class T, int W, bool TINY>
 struct att_lane {
   int lph;    // lanes per head
   int hk;     // key head (of a lane without one: the last)
   int c;      // first column of its vector within the head: the last vector of a head moves back to end with it
   int lo, hi; // elements [lo, hi) of the vector are its own (a moved-back vector's leading ones belong to the vector before)
-  float own[W], scaled[W];  // 1 or the scale for those, else 0
+  att_mask<T, W> mask;
   bool live, first;  // first: has the head's first column
   __device__ __forceinline__ att_lane(const att_args& a, int q, int hb) {
     lph = a.lph;
@@ -48,10 +71,7 @@ struct att_lane {
     hi = TINY ? a.dh : W;
     first = live && c0 == 0;
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-      own[j] = j >= lo && j < hi ? 1.f : 0.f;
-      scaled[j] = j >= lo && j < hi ? a.scale : 0.f;
-    }
+    for (int j = 0; j < W; ++j) mask.set(j, j >= lo && j < hi, a.scale);
   }
   __device__ __forceinline__ int col(int head, int dh) const { return head * dh + c; }
 };
@@ -95,21 +115,68 @@ __device__ __forceinline__ void att_sums(float (&v)[N], int lph) {
 #undef ISP_STAGE
 }
 
+// A row operand's vector as a lane multiplies it with gathered ones: elements that are not its own count for nothing in a dot product.  (They are of
+// the same head, or the head is nobody's: an infinity or NaN among the gathered ones is in the dot product anyway.)
+// fp32: floats, with the scale in those of the scores.  16 bits: pairs as they lie, for the instruction that multiplies two pairs and adds both
+// products to a sum in 32 bits (exact products, subnormal numbers taken; less than 2^-21 of the terms off): half the instructions of fp32 from
+// fp16, less than half from bf16, which would have to be converted, and half the registers; the scale is then the score's.
+template <class T, int W>
+struct att_operand {
+  raw_t<T, W> v;
+  static constexpr bool SCALED = false;
+  __device__ __forceinline__ void set(const raw_t<T, W>& r, const att_mask<T, W>& m, bool) {
+    typedef typename att_mask<T, W>::bits bits;
+    v = __builtin_bit_cast(raw_t<T, W>, __builtin_bit_cast(bits, r) & m.keep);
+  }
+};
 template <int W>
-__device__ __forceinline__ float att_dot(const float (&a)[W], const float (&b)[W]) {
-  float s = a[0] * b[0];
+struct att_operand<float, W> {
+  float v[W];
+  static constexpr bool SCALED = true;
+  __device__ __forceinline__ void set(const raw_t<float, W>& r, const att_mask<float, W>& m, bool scaled) {
 #pragma unroll
-  for (int j = 1; j < W; ++j) s = fmaf(a[j], b[j], s);
+    for (int j = 0; j < W; ++j) v[j] = r[j] * (scaled ? m.scaled[j] : m.own[j]);
+  }
+};
+template <int W>
+__device__ __forceinline__ float att_dot(const att_operand<float, W>& a, const raw_t<float, W>& b) {
+  float s = a.v[0] * b[0];
+#pragma unroll
+  for (int j = 1; j < W; ++j) s = fmaf(a.v[j], b[j], s);
   return s;
 }
-// A lane's elements of a row operand times f, lane.own or lane.scaled: those that are not its own count for nothing in a dot product.  (They are of
-// the same head, or the head is nobody's: an infinity or NaN among them is in the dot product anyway.)
 template <class T, int W>
-__device__ __forceinline__ void att_own(const raw_t<T, W>& r, const float (&f)[W], float (&o)[W]) {
-  to_float<T, W>(r, o);
+__device__ __forceinline__ float att_dot(const att_operand<T, W>& a, const raw_t<T, W>& b) {
+  typedef T pair __attribute__((ext_vector_type(2)));
+  float s = 0.f;
 #pragma unroll
-  for (int j = 0; j < W; ++j) o[j] *= f[j];
+  for (int j = 0; j < W; j += 2) {
+    const pair x = {a.v[j], a.v[j + 1]}, y = {b[j], b[j + 1]};
+    if constexpr (__is_same(T, f16_t)) s = __builtin_amdgcn_fdot2(x, y, s, false);
+    else s = __builtin_amdgcn_fdot2_f32_bf16(x, y, s, false);
+  }
+  return s;
 }
+// Makes scores of N query heads' sums of products, but for the factor that is returned (the scale, where neither the operands have it nor a bias was added).
+// mask(out): the entry counts for nothing where `out`.
+template <class Operand, int BIAS, int N, int M, class Mask>
+__device__ __forceinline__ float att_scores(const att_args& a, float (&z)[M], float bias, Mask&& mask) {
+  const bool biased = BIAS == ATT_ASK ? a.bias : BIAS == ATT_BIAS;
+  if (biased) {
+    const bool out = bias == NEG_INF;
+#pragma unroll
+    for (int r = 0; r < N; ++r) z[r] = Operand::SCALED ? z[r] + bias : fmaf(z[r], a.scale, bias);
+    if (__any(out)) {
+#pragma unroll
+      for (int r = 0; r < N; ++r) z[r] = out ? NEG_INF : z[r];
+      mask(out);
+    }
+  }
+  return Operand::SCALED || biased ? 1.f : a.scale;
+}
+// ... and its distance to m
+template <class Operand>
+__device__ __forceinline__ float att_gap(float z, float f, float m) { return Operand::SCALED ? z - m : fmaf(z, f, -m); }
 
 // 1 / l by the hardware's reciprocal (about 1 ulp); 0 where the row has nothing.
 __device__ __forceinline__ float att_inverse(float l) { return l == 0.f ? 0.f : __builtin_amdgcn_rcpf(l); }
@@ -126,11 +193,12 @@ struct att_fwd {
   static constexpr int W = W_, RQ = RQ_, RING = 4, PARTS = RQ, MOST = 4;
   static constexpr bool WIDE = true;
   static constexpr bool TINY = TINY_;
-  using lane_t = att_lane<W, TINY>;
+  using lane_t = att_lane<T, W, TINY>;
+  using operand = att_operand<T, W>;
   struct gathered { raw_t<T, W> k, v; };
   struct source { const T *k, *v; };  // the lane's columns of row 0
   struct requested { raw_t<T, W> q[RQ]; };
-  struct row_t { float q[RQ][W]; };
+  struct row_t { operand q[RQ]; };
   struct part { float y[W], m, l; };  // of a query head
 
   static __device__ __forceinline__ int head(const att_args& a, const lane_t& ln, int r) { return ln.hk * a.group + (int)blockIdx.z * RQ + r; }
@@ -155,44 +223,36 @@ struct att_fwd {
   }
   static __device__ __forceinline__ void row(const att_args& a, const lane_t& ln, const requested& o, row_t& w) {
 #pragma unroll
-    for (int r = 0; r < RQ; ++r) att_own<T, W>(o.q[r], ln.scaled, w.q[r]);
+    for (int r = 0; r < RQ; ++r) w.q[r].set(o.q[r], ln.mask, true);
   }
-  template <int LPG>
+  template <int LPG, int BIAS>
   static __device__ __forceinline__ void edge(const att_args& a, const lane_t& ln, float bias, const gathered& g, const row_t& w, part (&s)[PARTS]) {
-    float k[W], v[W], z[RQ];
-    to_float<T, W>(g.k, k);
+    float v[W], z[RQ];
     to_float<T, W>(g.v, v);
 #pragma unroll
-    for (int r = 0; r < RQ; ++r) z[r] = att_dot<W>(w.q[r], k);
+    for (int r = 0; r < RQ; ++r) z[r] = att_dot(w.q[r], g.k);
     att_sums<LPG, RQ>(z, ln.lph);
-    if (a.bias) {
-      const bool out = bias == NEG_INF;
+    const float f = att_scores<operand, BIAS, RQ>(a, z, bias, [&](bool out) {  // (whatever its operands hold)
 #pragma unroll
-      for (int r = 0; r < RQ; ++r) z[r] += bias;
-      if (__any(out)) {  // (whatever their operands hold)
-#pragma unroll
-        for (int r = 0; r < RQ; ++r) z[r] = out ? NEG_INF : z[r];
-#pragma unroll
-        for (int j = 0; j < W; ++j) v[j] = out ? 0.f : v[j];
-      }
-    }
+      for (int j = 0; j < W; ++j) v[j] = out ? 0.f : v[j];
+    });
     float gap[RQ];
     bool move = false;
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
-      gap[r] = z[r] - s[r].m;
+      gap[r] = att_gap<operand>(z[r], f, s[r].m);
       move |= gap[r] > ATT_SLACK;
     }
     if (__any(move)) {
 #pragma unroll
       for (int r = 0; r < RQ; ++r) {
         const bool up = gap[r] > ATT_SLACK;
-        const float f = up ? fast_exp(-gap[r]) : 1.f;
-        s[r].m = up ? z[r] : s[r].m;
-        gap[r] = up ? z[r] - z[r] : gap[r];  // (0; +inf: NaN)
-        s[r].l *= f;
+        const float less = up ? fast_exp(-gap[r]) : 1.f, to = operand::SCALED ? z[r] : z[r] * f;
+        s[r].m = up ? to : s[r].m;
+        gap[r] = up ? to - to : gap[r];  // (0; +inf: NaN)
+        s[r].l *= less;
 #pragma unroll
-        for (int j = 0; j < W; ++j) s[r].y[j] *= f;
+        for (int j = 0; j < W; ++j) s[r].y[j] *= less;
       }
     }
 #pragma unroll
@@ -228,6 +288,8 @@ struct att_fwd {
       }
     }
   }
+  static __device__ __forceinline__ void store(const att_args& a, const lane_t& ln, int row, const part (&s)[PARTS], const row_t&) { store(a, ln, row, s); }
+  static __device__ __forceinline__ void store_empty(const att_args& a, const lane_t& ln, int row, const part (&s)[PARTS]) { store(a, ln, row, s); }
   // a segment's partial row: heads * dh sums, then (m, l) of each head
   static __device__ __forceinline__ void store_part(const att_args& a, const lane_t& ln, int seg, const part (&s)[PARTS]) {
     if (!ln.live) return;
@@ -245,14 +307,6 @@ struct att_fwd {
 };
 
 // ---- backward ------------------------------------------------------------------------------------------------------
-// The numbers of a row and head that the columns' pass reads: reference, 1 / l, D.
-__device__ __forceinline__ void att_leave(const att_args& a, int row, int h, float d) {
-  const int64_t at = (int64_t)row * a.heads + h;
-  a.stat[at] = {a.stats[2 * at], att_inverse(a.stats[2 * at + 1]), d, 0.f};
-}
-// P of a score z whose row has numbers st
-__device__ __forceinline__ float att_weight(float z, const att_num& st) { return fast_exp(z - st.m) * st.inv; }
-
 // over A's rows: dq, and D
 template <class T_, int W_, int RQ_, bool TINY_>
 struct att_bwd_row {
@@ -260,12 +314,13 @@ struct att_bwd_row {
   static constexpr int W = W_, RQ = RQ_, RING = 4, PARTS = RQ, MOST = 2;
   static constexpr bool WIDE = false;
   static constexpr bool TINY = TINY_;
-  using lane_t = att_lane<W, TINY>;
+  using lane_t = att_lane<T, W, TINY>;
+  using operand = att_operand<T, W>;
   struct gathered { raw_t<T, W> k, v; };
   struct source { const T *k, *v; };
   struct requested { raw_t<T, W> q[RQ], dy[RQ]; float2 ml[RQ]; };
-  struct row_t { float q[RQ][W], dy[RQ][W]; att_num st[RQ]; };
-  struct part { float pt[W], p[W], d; };  // of a query head: sums of P t k, P k and P t
+  struct row_t { operand q[RQ], dy[RQ]; float m[RQ], l[RQ]; };
+  struct part { float pt[W], p[W], d; };  // of a query head, e = exp(s - m): sums of e t k, e k and e t
 
   static __device__ __forceinline__ int head(const att_args& a, const lane_t& ln, int r) { return ln.hk * a.group + (int)blockIdx.z * RQ + r; }
   static __device__ __forceinline__ void clear(part& s) {
@@ -295,39 +350,31 @@ struct att_bwd_row {
   static __device__ __forceinline__ void row(const att_args& a, const lane_t& ln, const requested& o, row_t& w) {
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
-      att_own<T, W>(o.q[r], ln.scaled, w.q[r]);
-      att_own<T, W>(o.dy[r], ln.own, w.dy[r]);
-      w.st[r] = {o.ml[r].x, att_inverse(o.ml[r].y), 0.f, 0.f};
+      w.q[r].set(o.q[r], ln.mask, true);
+      w.dy[r].set(o.dy[r], ln.mask, false);
+      w.m[r] = o.ml[r].x;
+      w.l[r] = o.ml[r].y;
     }
   }
-  template <int LPG>
+  template <int LPG, int BIAS>
   static __device__ __forceinline__ void edge(const att_args& a, const lane_t& ln, float bias, const gathered& g, const row_t& w, part (&s)[PARTS]) {
-    float k[W], v[W], z[2 * RQ];
+    float k[W], z[2 * RQ];
     to_float<T, W>(g.k, k);
-    to_float<T, W>(g.v, v);
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
-      z[r] = att_dot<W>(w.q[r], k);
-      z[RQ + r] = att_dot<W>(w.dy[r], v);
+      z[r] = att_dot(w.q[r], g.k);
+      z[RQ + r] = att_dot(w.dy[r], g.v);
     }
     att_sums<LPG, 2 * RQ>(z, ln.lph);
-    if (a.bias) {
-      const bool out = bias == NEG_INF;
+    const float f = att_scores<operand, BIAS, RQ>(a, z, bias, [&](bool out) {
 #pragma unroll
-      for (int r = 0; r < RQ; ++r) z[r] += bias;
-      if (__any(out)) {
+      for (int r = 0; r < RQ; ++r) z[RQ + r] = out ? 0.f : z[RQ + r];
 #pragma unroll
-        for (int r = 0; r < RQ; ++r) {
-          z[r] = out ? NEG_INF : z[r];
-          z[RQ + r] = out ? 0.f : z[RQ + r];
-        }
-#pragma unroll
-        for (int j = 0; j < W; ++j) k[j] = out ? 0.f : k[j];
-      }
-    }
+      for (int j = 0; j < W; ++j) k[j] = out ? 0.f : k[j];
+    });
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
-      const float p = att_weight(z[r], w.st[r]), pt = p * z[RQ + r];
+      const float p = fast_exp(att_gap<operand>(z[r], f, w.m[r])), pt = p * z[RQ + r];
       s[r].d += pt;
 #pragma unroll
       for (int j = 0; j < W; ++j) {
@@ -344,19 +391,35 @@ struct att_bwd_row {
       s.p[j] += o.p[j];
     }
   }
+  static __device__ __forceinline__ void store_head(const att_args& a, const lane_t& ln, int row, int h, const part& s, float m, float inv) {
+    const float d = s.d * inv, f = a.scale * inv;
+    float o[W];
+#pragma unroll
+    for (int j = 0; j < W; ++j) o[j] = (s.pt[j] - d * s.p[j]) * f;
+    if (a.y) att_store<T, W, TINY>(static_cast<T*>(a.y) + (int64_t)row * a.ldy + ln.col(h, a.dh), a.dh, o);
+    if (ln.first) a.stat[(int64_t)row * a.heads + h] = {m, inv, d, 0.f};
+  }
   static __device__ __forceinline__ void store(const att_args& a, const lane_t& ln, int row, const part (&s)[PARTS]) {
     if (!ln.live) return;
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
-      const int h = head(a, ln, r);
-      float o[W];
-#pragma unroll
-      for (int j = 0; j < W; ++j) o[j] = (s[r].pt[j] - s[r].d * s[r].p[j]) * a.scale;
-      if (a.y) att_store<T, W, TINY>(static_cast<T*>(a.y) + (int64_t)row * a.ldy + ln.col(h, a.dh), a.dh, o);
-      if (ln.first) att_leave(a, row, h, s[r].d);
+      const float* st = a.stats + ((int64_t)row * a.heads + head(a, ln, r)) * 2;
+      store_head(a, ln, row, head(a, ln, r), s[r], st[0], att_inverse(st[1]));
     }
   }
-  // a segment's partial row: heads * dh sums of P t k, as many of P k, heads of P t
+  // (the row at work: its numbers are here, and loading them would wait for every gather in flight)
+  static __device__ __forceinline__ void store(const att_args& a, const lane_t& ln, int row, const part (&s)[PARTS], const row_t& w) {
+    if (!ln.live) return;
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) store_head(a, ln, row, head(a, ln, r), s[r], w.m[r], att_inverse(w.l[r]));
+  }
+  static __device__ __forceinline__ void store_empty(const att_args& a, const lane_t& ln, int row, const part (&)[PARTS]) {
+    if (!ln.live || !a.y) return;  // (nobody asks for the numbers of a row without entries)
+    const float o[W] = {};
+#pragma unroll
+    for (int r = 0; r < RQ; ++r) att_store<T, W, TINY>(static_cast<T*>(a.y) + (int64_t)row * a.ldy + ln.col(head(a, ln, r), a.dh), a.dh, o);
+  }
+  // a segment's partial row: heads * dh sums of e t k, as many of e k, heads of e t
   static __device__ __forceinline__ void store_part(const att_args& a, const lane_t& ln, int seg, const part (&s)[PARTS]) {
     if (!ln.live) return;
     const int width = a.heads * a.dh;
@@ -386,11 +449,12 @@ struct att_bwd_col {
   static constexpr int W = W_, RQ = RQ_, RING = RQ == 1 ? 4 : 2, PARTS = 1, MOST = 4;
   static constexpr bool WIDE = false;
   static constexpr bool TINY = TINY_;
-  using lane_t = att_lane<W, TINY>;
+  using lane_t = att_lane<T, W, TINY>;
+  using operand = att_operand<T, W>;
   struct gathered { raw_t<T, W> q[RQ], dy[RQ]; att_num st[RQ]; };
   struct source { const T *q, *dy; const att_num* st; };
   struct requested { raw_t<T, W> k, v; };
-  struct row_t { float k[W], v[W]; };
+  struct row_t { operand k, v; };
   struct part { float dk[W], dv[W]; };
 
   static __device__ __forceinline__ void clear(part& s) {
@@ -417,42 +481,34 @@ struct att_bwd_col {
     o.v = att_load<T, W, TINY>(att_row<T>(a.v, row, a.pv) + at, a.dh);
   }
   static __device__ __forceinline__ void row(const att_args& a, const lane_t& ln, const requested& o, row_t& w) {
-    att_own<T, W>(o.k, ln.scaled, w.k);
-    att_own<T, W>(o.v, ln.own, w.v);
+    w.k.set(o.k, ln.mask, true);
+    w.v.set(o.v, ln.mask, false);
   }
-  template <int LPG>
+  template <int LPG, int BIAS>
   static __device__ __forceinline__ void edge(const att_args& a, const lane_t& ln, float bias, const gathered& g, const row_t& w, part (&s)[PARTS]) {
     float q[RQ][W], dy[RQ][W], z[2 * RQ];
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
       to_float<T, W>(g.q[r], q[r]);
       to_float<T, W>(g.dy[r], dy[r]);
-      z[r] = att_dot<W>(w.k, q[r]);
-      z[RQ + r] = att_dot<W>(w.v, dy[r]);
+      z[r] = att_dot(w.k, g.q[r]);
+      z[RQ + r] = att_dot(w.v, g.dy[r]);
     }
     att_sums<LPG, 2 * RQ>(z, ln.lph);
-    if (a.bias) {
-      const bool out = bias == NEG_INF;
+    const float f = att_scores<operand, BIAS, RQ>(a, z, bias, [&](bool out) {
 #pragma unroll
-      for (int r = 0; r < RQ; ++r) z[r] += bias;
-      if (__any(out)) {
+      for (int r = 0; r < RQ; ++r) {
+        z[RQ + r] = out ? 0.f : z[RQ + r];
 #pragma unroll
-        for (int r = 0; r < RQ; ++r) {
-          z[r] = out ? NEG_INF : z[r];
-          z[RQ + r] = out ? 0.f : z[RQ + r];
+        for (int j = 0; j < W; ++j) {
+          q[r][j] = out ? 0.f : q[r][j];
+          dy[r][j] = out ? 0.f : dy[r][j];
         }
-#pragma unroll
-        for (int r = 0; r < RQ; ++r)
-#pragma unroll
-          for (int j = 0; j < W; ++j) {
-            q[r][j] = out ? 0.f : q[r][j];
-            dy[r][j] = out ? 0.f : dy[r][j];
-          }
       }
-    }
+    });
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
-      const float p = att_weight(z[r], g.st[r]), ds = p * (z[RQ + r] - g.st[r].d);
+      const float p = fast_exp(att_gap<operand>(z[r], f, g.st[r].m)) * g.st[r].inv, ds = p * (z[RQ + r] - g.st[r].d);
 #pragma unroll
       for (int j = 0; j < W; ++j) {
         s[0].dk[j] = fmaf(ds, q[r][j], s[0].dk[j]);
@@ -488,6 +544,8 @@ struct att_bwd_col {
         }
     }
   }
+  static __device__ __forceinline__ void store(const att_args& a, const lane_t& ln, int row, const part (&s)[PARTS], const row_t&) { store(a, ln, row, s); }
+  static __device__ __forceinline__ void store_empty(const att_args& a, const lane_t& ln, int row, const part (&s)[PARTS]) { store(a, ln, row, s); }
   // a segment's partial row: dk, then dv
   static __device__ __forceinline__ void store_part(const att_args& a, const lane_t& ln, int seg, const part (&s)[PARTS]) {
     if (!ln.live) return;
@@ -526,13 +584,13 @@ __global__ void __launch_bounds__(ISP_WG) k_att(isp_view A, const int64_t* __res
     P::clear(st[k]);
     P::clear(head[k]);
   }
-  for (int i = g; i < R.n_empty; i += G) P::store(a, ln, L.dst[RN_EMPTY0 - i], st);
+  for (int i = g; i < R.n_empty; i += G) P::store_empty(a, ln, L.dst[RN_EMPTY0 - i], st);
 
   if (R.steps == 0) return;  // (no entries: the operands may not be there)
 
   bool carried = R.mid, ended = false;
   const typename P::source src = P::sources(a, ln);
-  auto run = [&](auto seg_tag) {
+  auto run = [&](auto seg_tag, auto bias_tag) {
     constexpr bool SEG = decltype(seg_tag)::value;
     typename P::gathered x[RING];
     typename P::requested next;  // the row after the one at work, requested when that one began
@@ -542,9 +600,9 @@ __global__ void __launch_bounds__(ISP_WG) k_att(isp_view A, const int64_t* __res
     if constexpr (!SEG) P::request(a, ln, L.dst[R.k + 1], next);
     rn_stream<RING, !SEG, false, CHUNK>(
         L, R, [&](int u, int c, int, int, bool) { P::gather(a, src, c, x[u]); },
-        [&](auto u, float b, int) { P::template edge<LPG>(a, ln, b, x[u], cur, st); },
+        [&](auto u, float b, int) { P::template edge<LPG, decltype(bias_tag)::value>(a, ln, b, x[u], cur, st); },
         [&](int k, int row) {
-          if (!carried) P::store(a, ln, row, st);
+          if (!carried) P::store(a, ln, row, st, cur);
           if (__any(carried)) {  // (once per run)
 #pragma unroll
             for (int i = 0; i < PARTS; ++i)
@@ -558,8 +616,13 @@ __global__ void __launch_bounds__(ISP_WG) k_att(isp_view A, const int64_t* __res
           P::request(a, ln, L.dst[k + 2], next);
         });
   };
-  if (it.is_seg) run(std::true_type{});
-  else run(std::false_type{});
+  auto both = [&](auto bias_tag) {
+    if (it.is_seg) run(std::true_type{}, bias_tag);
+    else run(std::false_type{}, bias_tag);
+  };
+  if constexpr (P::W == 4) both(std::integral_constant<int, ATT_ASK>{});
+  else if (a.bias) both(std::integral_constant<int, ATT_BIAS>{});
+  else both(std::integral_constant<int, ATT_PLAIN>{});
 
   if (it.is_seg) {  // one row: the groups' parts
 #pragma unroll
@@ -684,8 +747,10 @@ __global__ void __launch_bounds__(ISP_WG) k_att_row_fixup(isp_view A, att_args a
 #pragma unroll
     for (int i = 1; i < ISP_WAVES_PER_WG; ++i) t[k] += part[i][k][lane];
   }
-  if (a.y) static_cast<T*>(a.y)[(int64_t)row * a.ldy + col] = (T)((t[0] - t[2] * t[1]) * a.scale);
-  if (col == h * a.dh) att_leave(a, row, h, t[2]);
+  const int64_t at = (int64_t)row * a.heads + h;
+  const float inv = att_inverse(a.stats[2 * at + 1]), d = t[2] * inv;
+  if (a.y) static_cast<T*>(a.y)[(int64_t)row * a.ldy + col] = (T)((t[0] - d * t[1]) * (a.scale * inv));
+  if (col == h * a.dh) a.stat[at] = {a.stats[2 * at], inv, d, 0.f};
 }
 template <class T>
 __global__ void __launch_bounds__(ISP_WG) k_att_col_fixup(isp_view A, att_args a) {
