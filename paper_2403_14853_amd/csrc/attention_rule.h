@@ -12,7 +12,7 @@ inline int att_lanes_per_head(int dh, int w) {
 }
 
 // Query heads of a key head that a lane takes at once: as many of `most` (4 or 2) as divide them.  The forward and the columns' pass take four, which reads
-// the gathered rows once for all; the rows' pass two, as four of them need 218 registers in 16 bits and spill in fp32.  us with four / two: 1 M rows, 17 M entries, 8 query
+// the gathered rows once for all; the rows' pass two, as four of them need 220 registers in 16 bits and 270 in fp32.  us with four / two: 1 M rows, 17 M entries, 8 query
 // heads on 2 of 16, bf16: forward 720 / 884, rows 1113 / 1142, columns 1294 / 2364 (in two passes); rows, fp16 1094 / 1140; 169 k, 2.4 M, fp32 325 / 249; 60 k, 6 M, 4 on 1 of 64, bf16 568 / 517, fp32
 // 1010 / 695.
 inline int att_share(int group, int most) { return group % 4 == 0 && most == 4 ? 4 : group % 2 == 0 ? 2 : 1; }

@@ -305,3 +305,24 @@ def test_many_heads(heads, kv, c, dtype):
     att.check_all(att.run(att.build(indptr, cols, m), q, k, v, dy, heads, kv), att.reference(indptr, cols, q, k, v, dy, heads, kv, c ** -0.5))
     with pytest.raises(isp.IspError):
         isp.attention(att.build(indptr, cols, m), *(torch.zeros(r, 4097 * 2, device="cuda") for r in (n, m, m, n)), 4097)
+
+
+@pytest.mark.parametrize("heads,kv,c", [(4, 2, 12), (3, 3, 20), (2, 1, 64), (1, 1, 3)])
+@pytest.mark.parametrize("small,large", [(2.0 ** -20, 2.0 ** 12), (2.0 ** 12, 2.0 ** -20), (2.0 ** 13, 2.0 ** 13)])
+def test_fp16_at_the_ends_of_its_range(heads, kv, c, small, large):
+    """Queries, or keys and values, that are subnormal in fp16, and products that fp16 could not hold: what the sums take of them is exact."""
+    n, m = 300, 250
+    indptr, cols = att.graph(n, m, 12)
+    q, k, v, dy = (t.float() for t in att.operands(n, m, heads, kv, c, torch.float16))
+    scale = 1 / (small * large * c ** 0.5)
+    both = small == large  # (then the gradients of values of 2^13 each would not fit: the small ones of V and dY)
+    q, k, v, dy = (t.half() for t in (q * small, k * large, v * (1 if both else large * 2.0 ** -4), dy * (2.0 ** -4 if both else small * 2.0 ** -2)))
+    if not both:
+        sub = q if small < large else k
+        assert ((sub != 0) & (sub.abs() < 2.0 ** -14)).float().mean() > 0.95  # (one in 40 is below half the smallest number, 2^-25)
+    got = att.run(att.build(indptr, cols, m), q, k, v, dy, heads, kv, scale=scale)
+    ref = att.reference(indptr, cols, q, k, v, dy, heads, kv, scale)
+    for name in ("y", "dq", "dk", "dv"):
+        if ref[name][0].abs().max() < 6e4:  # (fp16's largest number is 65504)
+            att.check(got[name], ref, name)
+    assert ref["y"][0].abs().max() < 6e4 and ref["dv"][0].abs().max() < 6e4
