@@ -191,7 +191,7 @@ template <class T_, int W_, int RQ_, bool TINY_>
 struct att_fwd {
   using T = T_;
   static constexpr int W = W_, RQ = RQ_, RING = 4, PARTS = RQ, MOST = 4;
-  static constexpr bool WIDE = true;
+  static constexpr bool WIDE = sizeof(T) == 2;
   static constexpr bool TINY = TINY_;
   using lane_t = att_lane<T, W, TINY>;
   using operand = att_operand<T, W>;
@@ -312,7 +312,7 @@ template <class T_, int W_, int RQ_, bool TINY_>
 struct att_bwd_row {
   using T = T_;
   static constexpr int W = W_, RQ = RQ_, RING = 4, PARTS = RQ, MOST = 2;
-  static constexpr bool WIDE = false;
+  static constexpr bool WIDE = sizeof(T) == 2;
   static constexpr bool TINY = TINY_;
   using lane_t = att_lane<T, W, TINY>;
   using operand = att_operand<T, W>;
@@ -446,8 +446,8 @@ __device__ __forceinline__ void att_out(const att_args& a, float* carry, T* out,
 template <class T_, int W_, int RQ_, bool TINY_>
 struct att_bwd_col {
   using T = T_;
-  static constexpr int W = W_, RQ = RQ_, RING = RQ == 1 ? 4 : 2, PARTS = 1, MOST = 4;
-  static constexpr bool WIDE = false;
+  static constexpr int W = W_, RQ = RQ_, RING = RQ == 1 && W == 4 ? 4 : 2, PARTS = 1, MOST = 4;
+  static constexpr bool WIDE = sizeof(T) == 2;
   static constexpr bool TINY = TINY_;
   using lane_t = att_lane<T, W, TINY>;
   using operand = att_operand<T, W>;
@@ -829,6 +829,11 @@ isp_status att_pass(const isp_view& v, att_args a, int rq, int chunks, bool wide
 }
 
 template <class T>
+bool att_takes_wide(const isp_csr* A, const att_args& a) {
+  return att_wide(sizeof(T), a.group, a.kv_heads, a.dh, A->info.nnz, A->info.n_rows - A->info.bin_rows[0]);
+}
+
+template <class T>
 isp_status att_forward(const isp_csr* A, att_args a, hipStream_t s) {
   const isp_view& v = A->v;
   const int rq = att_share(a.group, 4);
@@ -842,8 +847,7 @@ isp_status att_forward(const isp_csr* A, att_args a, hipStream_t s) {
     a.v = static_cast<const char*>(a.packed) + row_bytes;
     a.pk = a.pv = pitch;
   }
-  isp_status st = att_pass<att_fwd, T>(v, a, rq, a.group / rq,
-                                     att_wide(sizeof(T), a.group, a.kv_heads, a.dh, A->info.nnz, A->info.n_rows - A->info.bin_rows[0]), s);
+  isp_status st = att_pass<att_fwd, T>(v, a, rq, a.group / rq, att_takes_wide<T>(A, a), s);
   if (st != ISP_OK || v.n_hub == 0) return st;
   k_att_fwd_fixup<T><<<dim3((unsigned)v.n_hub, (unsigned)((a.heads * a.dh + ISP_WAVE - 1) / ISP_WAVE)), ISP_WG, 0, s>>>(v, a);
   ISP_LAUNCH_CHECK();
@@ -856,7 +860,7 @@ isp_status att_backward(const isp_csr* A, att_args a, const att_grads& o, hipStr
   const int rq_row = att_share(a.group, 2), rq = att_share(a.group, 4), passes = a.group / rq;
   a.y = o.dq;
   a.ldy = o.lddq;
-  isp_status st = att_pass<att_bwd_row, T>(v, a, rq_row, a.group / rq_row, false, s);
+  isp_status st = att_pass<att_bwd_row, T>(v, a, rq_row, a.group / rq_row, att_takes_wide<T>(A, a), s);
   if (st != ISP_OK) return st;
   if (v.n_hub > 0) {
     k_att_row_fixup<T><<<dim3((unsigned)v.n_hub, (unsigned)((a.heads * a.dh + ISP_WAVE - 1) / ISP_WAVE)), ISP_WG, 0, s>>>(v, a);
@@ -868,8 +872,9 @@ isp_status att_backward(const isp_csr* A, att_args a, const att_grads& o, hipStr
   a.y2 = o.dv;
   a.ldy2 = o.lddv;
   a.passes = passes;
+  const bool wide = att_takes_wide<T>(A->At, a);
   for (a.pass = 0; a.pass < passes; ++a.pass) {
-    if ((st = att_pass<att_bwd_col, T>(vt, a, rq, 1, false, s)) != ISP_OK) return st;
+    if ((st = att_pass<att_bwd_col, T>(vt, a, rq, 1, wide, s)) != ISP_OK) return st;
     if (vt.n_hub > 0) {
       k_att_col_fixup<T><<<dim3((unsigned)vt.n_hub, (unsigned)((2 * a.kv_heads * a.dh + ISP_WAVE - 1) / ISP_WAVE)), ISP_WG, 0, s>>>(vt, a);
       ISP_LAUNCH_CHECK();
