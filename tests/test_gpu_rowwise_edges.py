@@ -326,3 +326,18 @@ def test_fp16_at_the_ends_of_its_range(heads, kv, c, small, large):
         if ref[name][0].abs().max() < 6e4:  # (fp16's largest number is 65504)
             att.check(got[name], ref, name)
     assert ref["y"][0].abs().max() < 6e4 and ref["dv"][0].abs().max() < 6e4
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bfloat16", "float16"])
+@pytest.mark.parametrize("heads,c", [(8, 8), (3, 20), (2, 50), (1, 64), (1, 256), (16, 16), (5, 9), (70, 8)])
+def test_long_rows_in_16_bits(heads, c, dtype):
+    """Rows and columns of 30 entries on average: eight columns to a lane in every pass; with a bias that masks entries and whole rows, and without."""
+    n, m = 220, 200
+    indptr, cols = att.graph(n, m, 21, longest=60)
+    q, k, v, dy = att.operands(n, m, heads, heads, c, dtype)
+    att.check_all(att.run(att.build(indptr, cols, m), q, k, v, dy, heads, heads), att.reference(indptr, cols, q, k, v, dy, heads, heads, c ** -0.5))
+    bias = torch.randn(len(cols), generator=torch.Generator().manual_seed(2))
+    bias[::3] = -np.inf
+    bias[int(indptr[100]):int(indptr[104])] = -np.inf
+    got = att.run(att.build(indptr, cols, m, bias), q, k, v, dy, heads, heads, bias=True)
+    att.check_all(got, att.reference(indptr, cols, q, k, v, dy, heads, heads, c ** -0.5, bias))
