@@ -486,9 +486,11 @@ struct att_bwd_col {
   }
   template <int LPG, int BIAS>
   static __device__ __forceinline__ void edge(const att_args& a, const lane_t& ln, float bias, const gathered& g, const row_t& w, part (&s)[PARTS]) {
-    float q[RQ][W], dy[RQ][W], z[2 * RQ];
+    float q[RQ][W], dy[RQ][W], z[2 * RQ], inv[RQ], d[RQ];
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
+      inv[r] = g.st[r].inv;
+      d[r] = g.st[r].d;
       to_float<T, W>(g.q[r], q[r]);
       to_float<T, W>(g.dy[r], dy[r]);
       z[r] = att_dot(w.k, g.q[r]);
@@ -499,6 +501,8 @@ struct att_bwd_col {
 #pragma unroll
       for (int r = 0; r < RQ; ++r) {
         z[RQ + r] = out ? 0.f : z[RQ + r];
+        inv[r] = out ? 0.f : inv[r];  // (the row's numbers are not finite where one of its other entries is not)
+        d[r] = out ? 0.f : d[r];
 #pragma unroll
         for (int j = 0; j < W; ++j) {
           q[r][j] = out ? 0.f : q[r][j];
@@ -508,7 +512,7 @@ struct att_bwd_col {
     });
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
-      const float p = fast_exp(att_gap<operand>(z[r], f, g.st[r].m)) * g.st[r].inv, ds = p * (z[RQ + r] - g.st[r].d);
+      const float p = fast_exp(att_gap<operand>(z[r], f, g.st[r].m)) * inv[r], ds = p * (z[RQ + r] - d[r]);
 #pragma unroll
       for (int j = 0; j < W; ++j) {
         s[0].dk[j] = fmaf(ds, q[r][j], s[0].dk[j]);

@@ -467,3 +467,40 @@ def test_recorded_by_jit_trace():
         results.append((y.detach(), *torch.autograd.grad(y, leaves, dy)))
     for one, other in zip(*results):
         assert torch.equal(one, other)
+
+
+@pytest.mark.parametrize("heads,kv,c,dtype,wide", [(4, 2, 12, torch.float32, False), (8, 2, 16, torch.bfloat16, False), (2, 1, 3, torch.float16, False), (3, 3, 20, torch.float16, True),
+                                                   (8, 8, 16, torch.bfloat16, True), (6, 1, 8, torch.float32, False)])
+@pytest.mark.parametrize("where", ["q", "dy", "v"])
+def test_masked_entries_of_rows_that_are_not_finite(where, heads, kv, c, dtype, wide):
+    """Rows with masked entries and with others that make their sums infinite or NaN: the keys that such a row only reaches through masked entries have
+    the gradients of the row left out.  wide: rows of 16 entries and more on average, which 16-bit passes over one query head per key head take with eight
+    columns to a lane."""
+    n, m, bad = 90, 150, torch.tensor([11, 30, 55])
+    gen = np.random.default_rng(c)
+    lengths = gen.integers(20, 60, n) if wide else gen.integers(3, 9, n)
+    lengths[30] = 700  # (segments of a split row)
+    indptr = torch.zeros(n + 1, dtype=torch.int64)
+    indptr[1:] = torch.from_numpy(lengths).cumsum(0)
+    cols = torch.from_numpy(gen.integers(3, m, int(indptr[-1])).astype(np.int32))
+    rows = torch.repeat_interleave(torch.arange(n), torch.diff(indptr))
+    bias = torch.randn(len(cols), generator=torch.Generator().manual_seed(1))
+    mine = torch.isin(rows, bad)
+    bias[mine & (cols >= 30)] = -np.inf
+    for j, i in enumerate(bad.tolist()):  # the row's first entry counts, in a column that is its alone; the next one does not
+        at = int(indptr[i])
+        cols[at], bias[at] = j, 0.5
+        cols[at + 1], bias[at + 1] = 100 + j, -np.inf
+    q, k, v, dy = operands(n, m, heads, kv, c, dtype)
+    without = torch.where(mine, -np.inf, bias)
+    clean = reference(indptr, cols, q, k, v, dy, heads, kv, c ** -0.5, without)
+    values = torch.tensor([np.nan, np.inf, -np.inf], dtype=dtype, device="cuda")[:, None]
+    if where == "v":
+        v[:3] = values
+    else:
+        (q if where == "q" else dy)[bad.cuda()] = values
+    got = run(build(indptr, cols, m, bias), q, k, v, dy, heads, kv, bias=True)
+    outside, far = torch.ones(n, dtype=torch.bool), torch.arange(m) >= 30  # (columns below 30 may hold anything)
+    outside[bad] = False
+    for name, keep in (("y", outside), ("dq", outside), ("dk", far), ("dv", far)):
+        check(got[name][keep.cuda()], {name: tuple(t[keep] for t in clean[name])}, name)
