@@ -99,18 +99,19 @@ isp_status isp_attention(const isp_csr_t* A, const void* Q, int64_t ldq, const v
   ISP_TRY(check_operand(K, ldk, kv_heads * head_dim, live * A->v.n_cols, dtype, "K"));
   ISP_TRY(check_operand(V, ldv, kv_heads * head_dim, live * A->v.n_cols, dtype, "V"));
   ISP_TRY(isp_check_dense(Y, ldy, heads * head_dim, A->v.n_rows, "Y"));
-  ISP_TRY(check_workspace(workspace, workspace_bytes, forward_bytes(A, heads, head_dim)));
   const uint32_t size = dtype == ISP_F32 ? 4 : 2;
+  const auto lines = [&](const void* p, int64_t ld) { return (uintptr_t)p % isp_dev::ATT_LINE == 0 && ld * size % isp_dev::ATT_LINE == 0; };
+  const size_t parts = forward_bytes(A, heads, head_dim), copy = packed_bytes(A, kv_heads, head_dim, dtype, lines(K, ldk) && ldv == ldk && (uintptr_t)V % 4 == 0);
+  const bool pack = copy && workspace_bytes >= parts + copy;
+  ISP_TRY(check_workspace(workspace, workspace_bytes, parts + (pack ? copy : 0)));
   att_args a = make_args(heads, kv_heads, head_dim, scale, flags);
   a.q = Q, a.k = K, a.v = V;
   a.pq = (uint32_t)ldq * size, a.pk = (uint32_t)ldk * size, a.pv = (uint32_t)ldv * size;
   a.y = Y, a.ldy = ldy;
   a.stats = stats;
   a.part = static_cast<float*>(workspace);
-  const auto lines = [&](const void* p, int64_t ld) { return (uintptr_t)p % isp_dev::ATT_LINE == 0 && ld * size % isp_dev::ATT_LINE == 0; };
-  const size_t copy = packed_bytes(A, kv_heads, head_dim, dtype, lines(K, ldk) && ldv == ldk && (uintptr_t)V % 4 == 0);
-  if (copy && workspace_bytes >= forward_bytes(A, heads, head_dim) + copy) {
-    a.packed = static_cast<char*>(workspace) + forward_bytes(A, heads, head_dim);
+  if (pack) {
+    a.packed = static_cast<char*>(workspace) + parts;
     a.n_cols = A->v.n_cols;
   }
   if (dtype == ISP_F32) return isp_att_forward_f32(A, a, (hipStream_t)stream);

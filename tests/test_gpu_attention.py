@@ -7,6 +7,8 @@ most e u of itself, e = 40 + min(L, 800) + 40 max A over the entries that count.
 takes that on, and its sums over L entries the same number of half steps again.  Outputs are rounded once.  An exponential below 2^-126 is
 zero, and a row's sum is 1 or more (its reference is one of its scores): beside e u P every P may be off by 2^-126, which matters where a gradient is made
 of such entries alone (with scores of +-300: P = 5e-39 times t = 4 times q = 200 is 4e-36)."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -504,3 +506,35 @@ def test_masked_entries_of_rows_that_are_not_finite(where, heads, kv, c, dtype, 
     outside[bad] = False
     for name, keep in (("y", outside), ("dq", outside), ("dk", far), ("dv", far)):
         check(got[name][keep.cuda()], {name: tuple(t[keep] for t in clean[name])}, name)
+
+
+def test_workspace_without_split_rows():
+    """No row is split, so no partial rows are wanted; a workspace with room for the copy of K and V takes it, and has to be one."""
+    n, m, heads, c = 40_000, 600, 3, 20
+    indptr = torch.arange(n + 1) * 60
+    gen = torch.Generator().manual_seed(1)
+    cols = torch.randint(m, (60 * n,), generator=gen, dtype=torch.int32)
+    q, k, v, _ = operands(n, m, heads, heads, c, torch.float16)
+    A = isp.csr_build(indptr.cuda(), cols.cuda(), None, n_cols=m)
+    assert A.info()["n_segments"] == 0
+    need = isp.attention_workspace(A, heads, c, heads, torch.float16)
+    assert need == m * 256  # (two rows of 120 bytes in two lines)
+    y = torch.full_like(q, 7.0)
+    ws = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
+    p = lambda t: ctypes.c_void_p(t.data_ptr())
+    call = lambda ws, size: isp.load_library().isp_attention(A.handle, p(q), heads * c, p(k), heads * c, p(v), heads * c, heads, heads, c, ctypes.c_float(c ** -0.5), 0, 2,
+                                                             p(y), heads * c, None, ctypes.c_void_p(ws), size, None)
+    for bad in ((None, need), (None, 1 << 40), (ws.data_ptr() + 8, need), (ws.data_ptr() + 128, need)):
+        assert call(*bad) == 1  # ISP_EINVAL
+        torch.cuda.synchronize()
+        assert (y == 7).all()
+    results = []
+    for good in ((None, 0), (None, need - 1), (ws.data_ptr(), need), (ws.data_ptr() + 8, need - 1)):  # (with less than the copy takes nothing of it is used)
+        y.fill_(7)
+        torch.cuda.synchronize()
+        assert call(*good) == 0
+        torch.cuda.synchronize()
+        results.append(y.clone())
+    for r in results:
+        assert torch.equal(r, results[0])
+    assert (results[0] != 7).any(1).all()
