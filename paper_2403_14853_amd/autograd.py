@@ -37,6 +37,12 @@ class SparseGraph:
         return _b.csr_transpose_cached(self.handle)[0]
 
 
+def _values_without_gradient(graph: SparseGraph, what: str):
+    """Refuses where a gradient with respect to the edge values is asked for, which ``what`` does not have (under torch.no_grad() none is)."""
+    if graph.values is not None and graph.values.requires_grad and torch.is_grad_enabled():
+        raise NotImplementedError(what)
+
+
 class _Recorded(torch.autograd.Function):
     """One of the operations below while torch.jit.trace records a program: the native nodes are not among the operations
     that a recording knows (all that it would keep is the empty output they write into), an autograd function is."""
@@ -83,8 +89,7 @@ def matmul(graph: SparseGraph, X, reduce: str = "sum"):
         return spmm(graph, X)
     if reduce not in ("mean", "min", "max"):
         raise ValueError("reduce must be 'sum', 'mean', 'min' or 'max'")
-    if graph.values is not None and graph.values.requires_grad:
-        raise NotImplementedError("gradients with respect to the edge values exist for reduce='sum' only")
+    _values_without_gradient(graph, "gradients with respect to the edge values exist for reduce='sum' only")
     if _recorder() is not None:
         return _Recorded.apply(lambda _, X: _b._nat.ag_reduce(graph._native, X, _b.REDUCE[reduce]), None, X)
     return _b._nat.ag_reduce(graph._native, X, _b.REDUCE[reduce])
@@ -92,8 +97,7 @@ def matmul(graph: SparseGraph, X, reduce: str = "sum"):
 
 def fusedmm(graph: SparseGraph, X):
     """Differentiable sigmoid FusedMM: y_i = sum_j a_ij sigmoid(<x_i, x_j>) x_j (with respect to X only)."""
-    if graph.values is not None and graph.values.requires_grad:
-        raise NotImplementedError("FusedMM has no gradient with respect to the edge values")
+    _values_without_gradient(graph, "FusedMM has no gradient with respect to the edge values")
     if _recorder() is not None:
         return _Recorded.apply(lambda _, X: _b._nat.ag_fused(graph._native, X), None, X)
     return _b._nat.ag_fused(graph._native, X)
@@ -157,8 +161,8 @@ def attention(graph: SparseGraph, Q, K, V, heads: int, kv_heads=None, *, scale=N
     """Differentiable attention over the graph's entries (with respect to Q, K and V): per head, Y[i] = sum over row i's entries (i, j) of
     softmax(scale <Q[i], K[j]> (+ the entry's value with bias=True)) V[j].  Q [rows, heads * c], K, V [columns, kv_heads * c], fp32, bf16 or
     fp16; heads is a multiple of kv_heads (default: heads); scale: c ** -0.5 unless given."""
-    if bias and graph.values is not None and graph.values.requires_grad:
-        raise NotImplementedError("the attention has no gradient with respect to the edge values")
+    if bias:
+        _values_without_gradient(graph, "the attention has no gradient with respect to the edge values")
     kv_heads = heads if kv_heads is None else kv_heads
     scale = None if scale is None else float(scale)
     call = lambda Q, K, V: _b._nat.ag_attention(graph._native, Q, K, V, int(heads), int(kv_heads), scale, _b.ISP_BIAS_BY_A if bias else 0)

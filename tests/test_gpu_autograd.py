@@ -202,3 +202,20 @@ def test_second_backward_and_overwritten_input():
         else:
             Y.backward(dev(w.dY))
             assert_close(leaf.grad, *oracle.spmm(ti, tj, tv, w.dY), "after X was overwritten")
+
+
+def test_inference_with_trained_edge_values():
+    """Operations without a gradient with respect to the edge values refuse values that want one; where no gradient is asked for they run."""
+    from paper_2403_14853_amd import autograd as ag
+    w = graphgen.make_config(1, shrink=64)
+    X = dev(w.X)[:, :32].contiguous()
+    trained = ag.SparseGraph(dev(w.indptr), dev(w.indices), dev(w.values).requires_grad_(True))
+    plain = ag.SparseGraph(dev(w.indptr), dev(w.indices), dev(w.values))
+    for call in (lambda g: ag.matmul(g, X, "mean"), lambda g: ag.matmul(g, X, "max"), lambda g: ag.fusedmm(g, X), lambda g: ag.attention(g, X, X, X, 4, bias=True)):
+        with pytest.raises(NotImplementedError):
+            call(trained)
+        with torch.no_grad():
+            got = call(trained)
+        assert torch.equal(got, call(plain)) and not got.requires_grad
+        with torch.inference_mode():
+            assert torch.equal(call(trained), got)
