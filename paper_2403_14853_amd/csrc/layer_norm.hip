@@ -332,12 +332,13 @@ __global__ void __launch_bounds__(BT) k_ln_sums_any(ln_args a) {
   a.sums[((int64_t)blockIdx.y * 2 + 1) * a.d + c] = db;
 }
 
-// The workgroups' rows of sums, added up: 16 columns per workgroup, 64 threads to a column, each a run of consecutive rows.
+// The workgroups' rows of sums, added up: 16 columns per workgroup (from column col0 of dw's and dbias's on), 64 threads to a column, each a run of
+// consecutive rows.
 constexpr int LN_COLS = 16, LN_RUNS = 64;
-__global__ void __launch_bounds__(LN_COLS* LN_RUNS) k_ln_sums(const float* __restrict__ sums, int rows, int d, void* dw, void* db, int param) {
+__global__ void __launch_bounds__(LN_COLS* LN_RUNS) k_ln_sums(const float* __restrict__ sums, int rows, int d, void* dw, void* db, int param, int64_t col0) {
   __shared__ double part[LN_RUNS][LN_COLS];
   const int c = threadIdx.x % LN_COLS, r = threadIdx.x / LN_COLS;
-  const int64_t col = (int64_t)blockIdx.x * LN_COLS + c, cols = 2 * (int64_t)d;
+  const int64_t col = col0 + (int64_t)blockIdx.x * LN_COLS + c, cols = 2 * (int64_t)d;
   const int per = (rows + LN_RUNS - 1) / LN_RUNS;
   const int lo = r * per, hi = lo + per < rows ? lo + per : rows;
   double s = 0.;
@@ -451,8 +452,12 @@ isp_status isp_layer_norm_bwd_launch(const void* X, int64_t ldx, const void* dY,
     ISP_LAUNCH_CHECK();
   }
   if (sums) {  // (of no rows: zeros)
-    k_ln_sums<<<(unsigned)ceil_div(2 * (int64_t)d, LN_COLS), LN_COLS * LN_RUNS, 0, s>>>(static_cast<const float*>(ws), (int)(n > 0 ? ln_bwd_groups(n, d) : 0), d,
-                                                                                     dweight, dbias, param);
+    const int rows = n > 0 ? (int)ln_bwd_groups(n, d) : 0;
+    constexpr int64_t MOST = (1ll << 31) / LN_RUNS;  // columns of a launch, which has to stay below 2^32 threads
+    for (int64_t c0 = 0, cols = 2 * (int64_t)d; c0 < cols; c0 += MOST) {
+      const int64_t some = cols - c0 < MOST ? cols - c0 : MOST;
+      k_ln_sums<<<(unsigned)ceil_div(some, LN_COLS), LN_COLS * LN_RUNS, 0, s>>>(static_cast<const float*>(ws), rows, d, dweight, dbias, param, c0);
+    }
     ISP_LAUNCH_CHECK();
   }
   return ISP_OK;

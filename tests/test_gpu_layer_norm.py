@@ -265,3 +265,21 @@ def test_recorded_by_jit_trace():
         results.append((out.detach(), *torch.autograd.grad(out, (leaf, layer.w, layer.b), x)))
     for one, other in zip(*results):
         assert torch.equal(one, other)
+
+
+def test_gradients_of_more_columns_than_a_launch_has_threads_for():
+    """2^25 columns and more: the sums over the rows have 64 threads to each of twice as many columns.  dw is made of h, off by at most what the row's mean and
+    rstd of the forward are off by (both are handed over here), so two products and a sum: 4 half steps of the magnitudes."""
+    n, d = 2, (1 << 25) + 37
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    x, dy = (torch.randn(n, d, device="cuda", generator=gen) for _ in range(2))
+    mean, rstd = torch.tensor([0.25, -0.5], device="cuda"), torch.tensor([1.5, 0.75], device="cuda")
+    dw, db = torch.full((d,), 7.0, device="cuda"), torch.full((d,), 7.0, device="cuda")
+    isp.layer_norm_backward(x, dy, None, mean, rstd, None, dw, db)
+    h = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    u = 2.0 ** -24
+    terms = dy.double() * h
+    assert ((dw.double() - terms.sum(0)).abs() <= 4 * u * ((dy.double() * rstd.double()[:, None]).abs() * (x.double().abs() + mean.double().abs()[:, None])).sum(0)).all()
+    assert ((db.double() - dy.double().sum(0)).abs() <= 2 * u * dy.double().abs().sum(0)).all()
+    isp.layer_norm_backward(x[:0], dy[:0], None, mean[:0], rstd[:0], None, dw, db)
+    assert not dw.any() and not db.any()
