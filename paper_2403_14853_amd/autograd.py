@@ -4,6 +4,8 @@ forward and backward propagation to the kernels, Section 3.1).  Everything numer
 in the library's HIP kernels; the nodes (csrc/torch_native.cpp) only route tensors and remember what
 backward needs.
 
+There are no second derivatives: gradients made with ``create_graph=True`` raise NotImplementedError when they are differentiated.
+
 ``SparseGraph`` owns the handle; its transpose is built on the first backward and cached in the
 handle for all later epochs (Section 3.3).
 """
@@ -67,7 +69,7 @@ class _Recorded(torch.autograd.Function):
     def backward(ctx, dY):
         ctx.saved_tensors
         wanted = [t for t, need in zip(ctx.leaves, ctx.needs_input_grad[1:]) if need]
-        got = iter(torch.autograd.grad(ctx.output, wanted, dY, retain_graph=True))
+        got = iter(torch.autograd.grad(ctx.output, wanted, dY, retain_graph=True, create_graph=torch.is_grad_enabled()))
         return (None, *(next(got) if need else None for need in ctx.needs_input_grad[1:]))
 
 
@@ -135,7 +137,8 @@ class _RecordedRows(torch.autograd.Function):
         ctx.saved_tensors
         wanted = [t for t, need in zip(ctx.leaves, ctx.needs_input_grad[1:]) if need]
         pairs = [(o, g) for o, g in zip(ctx.outputs, grads) if o.requires_grad]
-        got = iter(torch.autograd.grad([o for o, _ in pairs], wanted, [g for _, g in pairs], retain_graph=True))
+        got = iter(torch.autograd.grad([o for o, _ in pairs], wanted, [g for _, g in pairs], retain_graph=True,
+                                       create_graph=torch.is_grad_enabled()))
         return (None, *(next(got) if need else None for need in ctx.needs_input_grad[1:]))
 
 

@@ -14,6 +14,7 @@
 #include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPStream.h>
 #include <hip/hip_runtime_api.h>
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <memory>
@@ -665,6 +666,38 @@ Cell& transpose(Graph& g) {
 
 Tensor new_like(const Tensor& t, int64_t rows, int64_t d) { return at::empty({rows, d}, t.options().requires_grad(false)); }
 
+// No gradient here has a derivative of its own.  Asked for gradients that can be differentiated again (create_graph), a node hands them out with
+// this one behind them, which says so to whoever goes through: otherwise their part of a second derivative would be lost without a word.
+struct NoSecondDerivative : torch::autograd::Node {
+  std::string name() const override { return "IspNoSecondDerivative"; }
+  variable_list apply(variable_list&&) override {
+    pybind11::gil_scoped_acquire gil;
+    PyErr_SetString(PyExc_NotImplementedError, "the gradients of the sparse operations, layer norm, attention and label log probabilities cannot be differentiated again");
+    python_error e;
+    e.persist();
+    throw python_error(std::move(e));
+  }
+};
+// In a node's apply, made before anything else: the mode in which the engine runs it, and a mode without recording.
+class Once {
+  const bool again_ = at::GradMode::is_enabled();
+  at::NoGradGuard no_grad_;
+
+ public:
+  // The gradients `out` of `grads`; by_input: they depend on the node's inputs, too.
+  variable_list operator()(torch::autograd::Node& node, const variable_list& grads, variable_list out, bool by_input) const {
+    if (!again_) return out;
+    torch::autograd::edge_list edges = by_input ? node.next_edges() : torch::autograd::edge_list();
+    for (const Tensor& g : grads)
+      if (g.defined() && g.requires_grad()) edges.push_back(torch::autograd::impl::gradient_edge(g));
+    if (std::none_of(edges.begin(), edges.end(), [](const torch::autograd::Edge& e) { return e.is_valid(); })) return out;
+    auto stop = std::shared_ptr<NoSecondDerivative>(new NoSecondDerivative(), torch::autograd::deleteNode);
+    stop->set_next_edges(std::move(edges));
+    torch::autograd::set_history(out, stop);
+    return out;
+  }
+};
+
 struct SpmmBackward : torch::autograd::Node {
   GraphPtr graph;
   torch::autograd::SavedVariable X;  // only where the values have a gradient
@@ -674,7 +707,7 @@ struct SpmmBackward : torch::autograd::Node {
   variable_list apply(variable_list&& grads) override {
     variable_list out(2);
     if (!grads[0].defined()) return out;
-    at::NoGradGuard no_grad;
+    const Once once;
     const Tensor dY = grads[0].contiguous();
     const Dense G = dense(dY);
     if (task_should_compute_output(1)) {
@@ -688,7 +721,7 @@ struct SpmmBackward : torch::autograd::Node {
       out[0] = at::empty({graph->A->nnz}, dY.options());
       run(*graph->A, [&](isp_csr_t* h, void* s) { return isp_sddmm(h, G.p, G.ld, V.p, V.ld, (int32_t)G.d, 0, static_cast<float*>(out[0].data_ptr()), s); });
     }
-    return out;
+    return once(*this, grads, std::move(out), need_dA);
   }
 };
 
@@ -700,7 +733,7 @@ struct ReduceBackward : torch::autograd::Node {
   variable_list apply(variable_list&& grads) override {
     variable_list out(1);
     if (!grads[0].defined()) return out;
-    at::NoGradGuard no_grad;
+    const Once once;
     transpose(*graph);  // built on the first backward, cached afterwards
     const Tensor dY = grads[0].contiguous();
     const Dense G = dense(dY);
@@ -709,7 +742,7 @@ struct ReduceBackward : torch::autograd::Node {
     run(*graph->A, [&](isp_csr_t* h, void* s) {
       return isp_spmm_reduce_backward(h, G.p, G.ld, (int32_t)G.d, reduce, arg.defined() ? static_cast<const int32_t*>(arg.data_ptr()) : nullptr, O.p, O.ld, s);
     });
-    return out;
+    return once(*this, grads, std::move(out), false);
   }
 };
 
@@ -721,14 +754,14 @@ struct FusedBackward : torch::autograd::Node {
   variable_list apply(variable_list&& grads) override {
     variable_list out(1);
     if (!grads[0].defined()) return out;
-    at::NoGradGuard no_grad;
+    const Once once;
     transpose(*graph);
     const Tensor x = X.unpack(), dY = grads[0].contiguous();
     const Dense V = dense(x), G = dense(dY);
     out[0] = new_like(x, V.rows, V.d);
     const Dense O = dense(out[0]);
     run(*graph->A, [&](isp_csr_t* h, void* s) { return isp_fusedmm_backward(h, V.p, V.ld, G.p, G.ld, (int32_t)V.d, ISP_OP_SIGMOID, O.p, O.ld, s); });
-    return out;
+    return once(*this, grads, std::move(out), true);
   }
 };
 
@@ -916,7 +949,7 @@ struct LayerNormBackward : torch::autograd::Node {
   variable_list apply(variable_list&& grads) override {
     variable_list out(3);
     if (!grads[0].defined()) return out;
-    at::NoGradGuard no_grad;
+    const Once once;
     const Tensor x = X.unpack(), w = weight.unpack(), dY = rows_of(grads[0]);
     const Mat M = mat(x), G = mat(dY);
     const Norm P = params(w, Tensor(), M);
@@ -937,7 +970,7 @@ struct LayerNormBackward : torch::autograd::Node {
     check(isp_layer_norm_backward(M.p, M.ld, G.p, G.ld, M.rows, (int32_t)M.d, M.type, P.w, type_of(param), mean.data_ptr<float>(), rstd.data_ptr<float>(),
                                   O.p, O.ld, out[1].defined() ? out[1].data_ptr() : nullptr, out[2].defined() ? out[2].data_ptr() : nullptr,
                                   ws.defined() ? ws.data_ptr() : nullptr, bytes, here().s));
-    return out;
+    return once(*this, grads, std::move(out), true);
   }
 };
 
@@ -1002,7 +1035,7 @@ struct LabelLogprobBackward : torch::autograd::Node {
   variable_list apply(variable_list&& grads) override {
     variable_list out(1);
     if (!grads[0].defined() && !grads[1].defined()) return out;
-    at::NoGradGuard no_grad;
+    const Once once;
     const Tensor z = Z.unpack(), y = labels.unpack(), e = entropy.unpack(shared_from_this());
     const Mat M = mat(z);
     const Tensor da = grads[0].defined() ? grads[0].contiguous() : Tensor(), de = grads[1].defined() ? grads[1].contiguous() : Tensor();
@@ -1011,7 +1044,7 @@ struct LabelLogprobBackward : torch::autograd::Node {
     check(isp_label_logprob_backward(M.p, M.ld, M.rows, (int32_t)M.d, M.type, static_cast<const int64_t*>(array(y, at::kLong, M.rows)), stats.data_ptr<float>(),
                                      static_cast<const float*>(array(e, at::kFloat, M.rows)), static_cast<const float*>(array(da, at::kFloat, M.rows)),
                                      static_cast<const float*>(array(de, at::kFloat, M.rows)), O.p, O.ld, here().s));
-    return out;
+    return once(*this, grads, std::move(out), true);
   }
 };
 
@@ -1083,7 +1116,7 @@ struct AttentionBackward : torch::autograd::Node {
   variable_list apply(variable_list&& grads) override {
     variable_list out(3);
     if (!grads[0].defined()) return out;
-    at::NoGradGuard no_grad;
+    const Once once;
     TORCH_CHECK(!(flags & ISP_BIAS_BY_A) || graph->values._version() == bias_version,
                 "the graph's values, which the attention's backward needs, have been modified by an inplace operation");
     const Tensor q = Q.unpack(), k = K.unpack(), v = V.unpack(), dY = rows_of(grads[0]);
@@ -1108,7 +1141,7 @@ struct AttentionBackward : torch::autograd::Node {
       return isp_attention_backward(h, MQ.p, MQ.ld, MK.p, MK.ld, MV.p, MV.ld, H.heads, H.kv, H.dim, scale, flags, MQ.type, stats.data_ptr<float>(),
                                     G.p, G.ld, O[0].p, O[0].ld, O[1].p, O[1].ld, O[2].p, O[2].ld, ws.data_ptr(), bytes, s);
     });
-    return out;
+    return once(*this, grads, std::move(out), true);
   }
 };
 

@@ -219,3 +219,45 @@ def test_inference_with_trained_edge_values():
         assert torch.equal(got, call(plain)) and not got.requires_grad
         with torch.inference_mode():
             assert torch.equal(call(trained), got)
+
+
+@pytest.mark.parametrize("op,traced", [(op, traced) for op in ("spmm", "values", "mean", "max", "fused", "norm", "labels", "attention") for traced in (False, True)
+                                       if (op, traced) != ("values", True)])  # (a trace takes no constant that wants a gradient)
+def test_second_derivatives_are_not_lost_without_a_word(op, traced):
+    """Gradients that are to be differentiated again are the same ones; whoever goes through them is told that it can't be done.  A gradient that depends on
+    nothing that is differentiated (a linear operation's, of a constant) has nothing to lose."""
+    from paper_2403_14853_amd import autograd as ag
+    w = graphgen.make_config(1, shrink=128)
+    n, d = w.n, 8
+    gen = torch.Generator().manual_seed(0)
+    r = lambda *s: torch.randn(*s, generator=gen).cuda()
+    values = dev(w.values).requires_grad_(op == "values")
+    g = ag.SparseGraph(dev(w.indptr), dev(w.indices), values)
+    labels = torch.randint(d, (n,), generator=gen).cuda()
+    run = {"spmm": lambda x: ag.spmm(g, x), "values": lambda x: ag.spmm(g, x), "mean": lambda x: ag.matmul(g, x, "mean"), "max": lambda x: ag.matmul(g, x, "max"),
+           "fused": lambda x: ag.fusedmm(g, x), "norm": lambda x: ag.layer_norm(x), "labels": lambda x: ag.label_logprob(x, labels)[0],
+           "attention": lambda x: ag.attention(g, x, x, x, 2)}[op]
+    if traced:
+        run = torch.jit.trace(run, (r(n, d),), check_trace=False)
+    linear = op in ("spmm", "mean", "max")
+    x = r(n, d).requires_grad_(True)
+    leaves = [x] + ([values] if op == "values" else [])
+    upstream = lambda y: (y * y).sum()  # (depends on the result)
+    plain = torch.autograd.grad(upstream(run(x)), leaves)
+    again = torch.autograd.grad(upstream(run(x)), leaves, create_graph=True)
+    for a, b in zip(plain, again):
+        assert torch.equal(a, b) and b.requires_grad and not a.requires_grad
+    with pytest.raises(NotImplementedError):
+        sum(t.sum() for t in again).backward()
+    if not traced:
+        again = torch.autograd.grad(upstream(run(x)), leaves, create_graph=True)
+        with pytest.raises(NotImplementedError):
+            torch.autograd.grad(again[0].sum(), x)
+    constant = r(n, d)[:, 0] if op == "labels" else r(n, d)
+    again = torch.autograd.grad(run(x), x, constant, create_graph=True)[0]
+    assert torch.equal(again, torch.autograd.grad(run(x), x, constant)[0])
+    assert again.requires_grad != linear
+    run(x).sum().backward(create_graph=True)  # (accumulated as it is)
+    run(x).sum().backward()
+    assert torch.isfinite(x.grad).all()
+    x.grad = None
