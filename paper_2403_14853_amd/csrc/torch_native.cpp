@@ -938,6 +938,7 @@ struct LayerNormBackward : torch::autograd::Node {
   SavedVariable X, weight;
   Tensor mean, rstd;
   bool bias = false;
+  std::vector<int64_t> bias_shape;  // (any shape of d elements)
   at::ScalarType param = at::kFloat;
   std::string name() const override { return "IspLayerNormBackward"; }
   void release_variables() override {
@@ -959,8 +960,8 @@ struct LayerNormBackward : torch::autograd::Node {
       O = mat(out[0]);
     }
     const auto like = x.options().dtype(param).requires_grad(false);
-    if (P.w && task_should_compute_output(1)) out[1] = at::empty({M.d}, like);
-    if (bias && task_should_compute_output(2)) out[2] = at::empty({M.d}, like);
+    if (P.w && task_should_compute_output(1)) out[1] = at::empty(w.sizes(), like);
+    if (bias && task_should_compute_output(2)) out[2] = at::empty(bias_shape, like);
     size_t bytes = 0;
     Tensor ws;
     if (out[1].defined() || out[2].defined()) {
@@ -1014,6 +1015,7 @@ PyObject* py_ag_layer_norm(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
       node->mean = mean;
       node->rstd = rstd;
       node->bias = b.defined();
+      if (b.defined()) node->bias_shape = b.sizes().vec();
       node->param = P.type == ISP_F32 ? at::kFloat : x.scalar_type();
       torch::autograd::set_history(Y, node);
     }

@@ -283,3 +283,17 @@ def test_gradients_of_more_columns_than_a_launch_has_threads_for():
     assert ((db.double() - dy.double().sum(0)).abs() <= 2 * u * dy.double().abs().sum(0)).all()
     isp.layer_norm_backward(x[:0], dy[:0], None, mean[:0], rstd[:0], None, dw, db)
     assert not dw.any() and not db.any()
+
+
+def test_parameters_of_any_shape():
+    """Weight and bias are d elements in any shape; their gradients have it, too."""
+    x, w, b, dy = make(40, 24, torch.float32, torch.float32)
+    leaves = [w.clone().requires_grad_(True), b.clone().requires_grad_(True)]
+    want = torch.autograd.grad(ag.layer_norm(x, *leaves), leaves, dy)
+    for ws, bs in (((1, 24), (24, 1)), ((2, 12), (24,)), ((24,), (4, 3, 2))):
+        leaves = [w.view(ws).clone().requires_grad_(True), b.view(bs).clone().requires_grad_(True)]
+        got = torch.autograd.grad(ag.layer_norm(x, *leaves), leaves, dy)
+        for g, t, leaf in zip(got, want, leaves):
+            assert g.shape == leaf.shape and torch.equal(g.flatten(), t)
+    only = b.view(2, 12).clone().requires_grad_(True)
+    assert torch.equal(torch.autograd.grad(ag.layer_norm(x, None, only), only, dy)[0].flatten(), want[1])
