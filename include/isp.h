@@ -329,6 +329,7 @@ isp_status isp_attention_workspace(const isp_csr_t* A, int32_t heads, int32_t kv
  *   Q, Y: n_rows x (heads * head_dim), K, V: n_cols x (kv_heads * head_dim), row-major, head after head; any ld (rows less than 4 GB apart) and
  *     any alignment that fits an element; dtype: ISP_F32 | ISP_BF16 | ISP_F16, of all four.  Scores, sums and products with P are held in 32 bits,
  *     Y is rounded once.  heads a multiple of kv_heads (at most 4096), head_dim <= 256.  Y must not overlap an operand.
+ *     Y's sums are formed before they are divided by the sum of exp(s - m), whose terms reach 3000: |V| times 3000 times the entries of a row has to fit fp32.
  *   stats: fp32, n_rows x heads x 2, written for the backward: a reference m for the row's scores and the sum of exp(s - m).  May be NULL.
  *   workspace: 256-byte aligned, of isp_attention_workspace bytes; used until the call's work on `stream` is done, nothing in it needs clearing.
  * Gathers are fastest from K and V that lie side by side in rows of whole 128-byte lines (column ranges of one projection's output).
@@ -350,6 +351,7 @@ isp_status isp_attention_backward_workspace(const isp_csr_t* A, int32_t heads, i
  * The column sums run over the rows of the cached transpose (Section 3.3), so isp_csr_transpose_cached(A) must have succeeded before - otherwise
  * ISP_EINVAL - unless dK and dV are NULL.  dQ, or dK and dV together, may be NULL: not wanted.  All of dtype, overwritten.
  * stats is what the forward wrote, with the same operands, scale, flags and values.  The scores are computed again, not read back.
+ * t_p K[j, g] and dS_p Q[i, h] have to fit fp32, as the results have; the weights P in these sums are at most 1.
  * There is no gradient with respect to the values.
  */
 isp_status isp_attention_backward(const isp_csr_t* A, const void* Q, int64_t ldq, const void* K, int64_t ldk,

@@ -1,7 +1,7 @@
 // Attention over the stored entries of a CSR matrix (gfx950, wave64): the three passes' kernels, instantiated per element type in attention_*.hip.
 //   forward   s_p = scale <q_i, k_j> + bias_p,  P = softmax over row i's entries,  y_i = sum_p P_p v_j           (p = (i, j))
 //   backward  t_p = <dy_i, v_j>,  D_i = sum_p P_p t_p,  dS_p = P_p (t_p - D_i)
-//             rows of A:    dq_i = scale sum_p dS_p k_j = scale / l_i (sum_p e_p t_p k_j - D_i sum_p e_p k_j),  e_p = exp(s_p - m_i) = P_p l_i
+//             rows of A:    dq_i = scale sum_p dS_p k_j = scale (sum_p P_p t_p k_j - D_i sum_p P_p k_j),  P_p = exp(s_p - m_i) / l_i
 //             rows of A^T:  dk_j = scale sum_p dS_p q_i,   dv_j = sum_p P_p dy_i
 // with `heads` query heads on `kv_heads` key heads: query head h reads key head h / R, R = heads / kv_heads.
 //
@@ -319,8 +319,8 @@ struct att_bwd_row {
   struct gathered { raw_t<T, W> k, v; };
   struct source { const T *k, *v; };
   struct requested { raw_t<T, W> q[RQ], dy[RQ]; float2 ml[RQ]; };
-  struct row_t { operand q[RQ], dy[RQ]; float m[RQ], l[RQ]; };
-  struct part { float pt[W], p[W], d; };  // of a query head, e = exp(s - m): sums of e t k, e k and e t
+  struct row_t { operand q[RQ], dy[RQ]; float m[RQ], inv[RQ]; };
+  struct part { float pt[W], p[W], d; };  // of a query head: sums of P t k, P k and P t
 
   static __device__ __forceinline__ int head(const att_args& a, const lane_t& ln, int r) { return ln.hk * a.group + (int)blockIdx.z * RQ + r; }
   static __device__ __forceinline__ void clear(part& s) {
@@ -353,7 +353,7 @@ struct att_bwd_row {
       w.q[r].set(o.q[r], ln.mask, true);
       w.dy[r].set(o.dy[r], ln.mask, false);
       w.m[r] = o.ml[r].x;
-      w.l[r] = o.ml[r].y;
+      w.inv[r] = att_inverse(o.ml[r].y);
     }
   }
   template <int LPG, int BIAS>
@@ -374,7 +374,7 @@ struct att_bwd_row {
     });
 #pragma unroll
     for (int r = 0; r < RQ; ++r) {
-      const float p = fast_exp(att_gap<operand>(z[r], f, w.m[r])), pt = p * z[RQ + r];
+      const float p = fast_exp(att_gap<operand>(z[r], f, w.m[r])) * w.inv[r], pt = p * z[RQ + r];  // (at most 1: what fits the operands' range fits the sums)
       s[r].d += pt;
 #pragma unroll
       for (int j = 0; j < W; ++j) {
@@ -392,12 +392,11 @@ struct att_bwd_row {
     }
   }
   static __device__ __forceinline__ void store_head(const att_args& a, const lane_t& ln, int row, int h, const part& s, float m, float inv) {
-    const float d = s.d * inv, f = a.scale * inv;
     float o[W];
 #pragma unroll
-    for (int j = 0; j < W; ++j) o[j] = (s.pt[j] - d * s.p[j]) * f;
+    for (int j = 0; j < W; ++j) o[j] = (s.pt[j] - s.d * s.p[j]) * a.scale;
     if (a.y) att_store<T, W, TINY>(static_cast<T*>(a.y) + (int64_t)row * a.ldy + ln.col(h, a.dh), a.dh, o);
-    if (ln.first) a.stat[(int64_t)row * a.heads + h] = {m, inv, d, 0.f};
+    if (ln.first) a.stat[(int64_t)row * a.heads + h] = {m, inv, s.d, 0.f};
   }
   static __device__ __forceinline__ void store(const att_args& a, const lane_t& ln, int row, const part (&s)[PARTS]) {
     if (!ln.live) return;
@@ -411,7 +410,7 @@ struct att_bwd_row {
   static __device__ __forceinline__ void store(const att_args& a, const lane_t& ln, int row, const part (&s)[PARTS], const row_t& w) {
     if (!ln.live) return;
 #pragma unroll
-    for (int r = 0; r < RQ; ++r) store_head(a, ln, row, head(a, ln, r), s[r], w.m[r], att_inverse(w.l[r]));
+    for (int r = 0; r < RQ; ++r) store_head(a, ln, row, head(a, ln, r), s[r], w.m[r], w.inv[r]);
   }
   static __device__ __forceinline__ void store_empty(const att_args& a, const lane_t& ln, int row, const part (&)[PARTS]) {
     if (!ln.live || !a.y) return;  // (nobody asks for the numbers of a row without entries)
@@ -419,7 +418,7 @@ struct att_bwd_row {
 #pragma unroll
     for (int r = 0; r < RQ; ++r) att_store<T, W, TINY>(static_cast<T*>(a.y) + (int64_t)row * a.ldy + ln.col(head(a, ln, r), a.dh), a.dh, o);
   }
-  // a segment's partial row: heads * dh sums of e t k, as many of e k, heads of e t
+  // a segment's partial row: heads * dh sums of P t k, as many of P k, heads of P t
   static __device__ __forceinline__ void store_part(const att_args& a, const lane_t& ln, int seg, const part (&s)[PARTS]) {
     if (!ln.live) return;
     const int width = a.heads * a.dh;
@@ -752,9 +751,8 @@ __global__ void __launch_bounds__(ISP_WG) k_att_row_fixup(isp_view A, att_args a
     for (int i = 1; i < ISP_WAVES_PER_WG; ++i) t[k] += part[i][k][lane];
   }
   const int64_t at = (int64_t)row * a.heads + h;
-  const float inv = att_inverse(a.stats[2 * at + 1]), d = t[2] * inv;
-  if (a.y) static_cast<T*>(a.y)[(int64_t)row * a.ldy + col] = (T)((t[0] - d * t[1]) * (a.scale * inv));
-  if (col == h * a.dh) a.stat[at] = {a.stats[2 * at], inv, d, 0.f};
+  if (a.y) static_cast<T*>(a.y)[(int64_t)row * a.ldy + col] = (T)((t[0] - t[2] * t[1]) * a.scale);
+  if (col == h * a.dh) a.stat[at] = {a.stats[2 * at], att_inverse(a.stats[2 * at + 1]), t[2], 0.f};
 }
 template <class T>
 __global__ void __launch_bounds__(ISP_WG) k_att_col_fixup(isp_view A, att_args a) {

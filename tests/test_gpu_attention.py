@@ -538,3 +538,15 @@ def test_workspace_without_split_rows():
     for r in results:
         assert torch.equal(r, results[0])
     assert (results[0] != 7).any(1).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["float32", "bfloat16"])
+@pytest.mark.parametrize("heads,kv,c", [(1, 1, 4), (4, 2, 12), (3, 3, 20)])
+def test_keys_of_large_magnitude(heads, kv, c, dtype):
+    """Keys of 2^117 and rows of up to 1,500 entries: dq is of the keys' size, and so has every sum on the way to be."""
+    n, m = 300, 250
+    indptr, cols = graph(n, m, 41)
+    q, k, v, dy = (t.float() for t in operands(n, m, heads, kv, c, dtype))
+    q, k = (q * 2.0 ** -114).to(dtype), (k * 2.0 ** 115).to(dtype)
+    scale = 1.5 / c ** 0.5
+    check_all(run(build(indptr, cols, m), q, k, v.to(dtype), dy.to(dtype), heads, kv, scale=scale), reference(indptr, cols, q, k, v, dy, heads, kv, scale))
