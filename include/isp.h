@@ -327,8 +327,9 @@ isp_status isp_attention_workspace(const isp_csr_t* A, int32_t heads, int32_t kv
  * Rows without entries, or with masked ones only: Y = 0.  An infinity or NaN in the operands of an entry that is not masked stays in its row and
  * head: one in Q or K may make them NaN (a score of +inf or NaN does), one in V makes its column infinite or NaN.
  *   Q, Y: n_rows x (heads * head_dim), K, V: n_cols x (kv_heads * head_dim), row-major, head after head; any ld (rows less than 4 GB apart) and
- *     any alignment that fits an element; dtype: ISP_F32 | ISP_BF16 | ISP_F16, of all four.  Scores, sums and products with P are held in 32 bits,
- *     Y is rounded once.  heads a multiple of kv_heads (at most 4096), head_dim <= 256.  Y must not overlap an operand.
+ *     any alignment that fits an element; dtype: ISP_F32 | ISP_BF16 | ISP_F16, of all four.  Scores, sums and products with P are held in 32 bits
+ *     (16-bit operands: dot products two columns at a time, each step off by up to 3 2^-24 of its terms, with subnormal operands counted as
+ *     the smallest normal number), Y is rounded once.  heads a multiple of kv_heads (at most 4096), head_dim <= 256.  Y must not overlap an operand.
  *     Y's sums are formed before they are divided by the sum of exp(s - m), whose terms reach 3000: |V| times 3000 times the entries of a row has to fit fp32.
  *   stats: fp32, n_rows x heads x 2, written for the backward: a reference m for the row's scores and the sum of exp(s - m).  May be NULL.
  *   workspace: 256-byte aligned, of isp_attention_workspace bytes; used until the call's work on `stream` is done, nothing in it needs clearing.

@@ -16,7 +16,7 @@
 // In the backward the rows' pass forms D beside dq's two sums, so that y, which has been rounded, is not needed, and leaves it to the
 // columns' pass.
 // Entries whose bias is -inf count for nothing, whatever their operands hold; a row without others has y = 0, l = 0.
-// Everything is held in 32 bits; outputs are rounded once.
+// Everything is held in 32 bits (dot products of 16-bit operands: att_operand); outputs are rounded once.
 #pragma once
 #include "attention_args.h"
 #include "elem.h"
@@ -118,8 +118,12 @@ __device__ __forceinline__ void att_sums(float (&v)[N], int lph) {
 // A row operand's vector as a lane multiplies it with gathered ones: elements that are not its own count for nothing in a dot product.  (They are of
 // the same head, or the head is nobody's: an infinity or NaN among the gathered ones is in the dot product anyway.)
 // fp32: floats, with the scale in those of the scores.  16 bits: pairs as they lie, for the instruction that multiplies two pairs and adds both
-// products to a sum in 32 bits (exact products, subnormal numbers taken; less than 2^-21 of the terms off): half the instructions of fp32 from
+// products to a sum in 32 bits: half the instructions of fp32 from
 // fp16, less than half from bf16, which would have to be converted, and half the registers; the scale is then the score's.
+// That instruction's result is off by at most 3 2^-24 of the three terms (2.9 in 10^6 random triples of like and of unlike magnitudes; .1 to .4 on
+// average, as much as two fused multiply-adds), in which a subnormal operand counts as the type's smallest normal number: products are lined up by
+// the operands' exponents as they are stored.  Next to a subnormal operand that is less than 2^-10 of what its own rounding to 16 bits is worth.  (fp16
+// with fused multiply-adds instead: 40 M entries, 3 heads of 20 917 / 961 us, 6 M, 2 of 128 with the backward 1222 / 1513.)
 template <class T, int W>
 struct att_operand {
   raw_t<T, W> v;

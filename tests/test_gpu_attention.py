@@ -550,3 +550,68 @@ def test_keys_of_large_magnitude(heads, kv, c, dtype):
     q, k = (q * 2.0 ** -114).to(dtype), (k * 2.0 ** 115).to(dtype)
     scale = 1.5 / c ** 0.5
     check_all(run(build(indptr, cols, m), q, k, v.to(dtype), dy.to(dtype), heads, kv, scale=scale), reference(indptr, cols, q, k, v, dy, heads, kv, scale))
+
+
+@pytest.mark.parametrize("heads,kv,c", [(4, 2, 12), (3, 3, 20), (1, 1, 3)])
+@pytest.mark.parametrize("dtype,large,small", [(torch.bfloat16, 2.0 ** 124, 2.0 ** -128), (torch.float16, 2.0 ** 12, 2.0 ** -16)], ids=["bfloat16", "float16"])
+def test_subnormal_operands(dtype, large, small, heads, kv, c):
+    """Keys that are mostly subnormal in their type, and queries that are too.  A sum of two products and a third term is off by at most 3 u of the terms, in which a subnormal operand counts as
+    the smallest normal number; up to 4 of those, 5 exchanges and the scale make 20 u A' of a score, A' = scale sum max(|q|, tiny) max(|k|, tiny), so
+    e = 40 + min(L, 800) + 44 max A' in place of the file's (its two differences of scores, and their rounding)."""
+    n, m = 300, 250
+    indptr, cols = graph(n, m, 31, longest=50)
+    tiny = torch.finfo(dtype).smallest_normal
+    for swap in (False, True):
+        q, k, v, dy = (t.float() for t in operands(n, m, heads, kv, c, dtype))
+        q, k = ((q * small, k * large) if swap else (q * large, k * small))
+        q, k, v, dy = (t.to(dtype) for t in (q, k, v, dy * 2.0 ** -6))
+        sub = q if swap else k
+        assert ((sub != 0) & (sub.abs() < tiny)).float().mean() > 0.8
+        scale = 1 / (small * large * c ** 0.5)
+        ref = reference(indptr, cols, q, k, v, dy, heads, kv, scale)
+        rows = torch.repeat_interleave(torch.arange(n), torch.diff(indptr))
+        long_row = torch.diff(indptr).clamp(max=800).double()
+        more = 1.0
+        for h in range(heads):
+            a, g = slice(h * c, h * c + c), slice(h // (heads // kv) * c, h // (heads // kv) * c + c)
+            Q, Kk = q[:, a].double().abs().cpu()[rows], k[:, g].double().abs().cpu()[cols.long()]
+            A, Am = scale * (Q * Kk).sum(1), scale * (Q.clamp(min=tiny) * Kk.clamp(min=tiny)).sum(1)
+            top = lambda x: torch.zeros(n, dtype=torch.float64).scatter_reduce(0, rows, x, "amax")
+            more = max(more, ((40 + long_row + 44 * top(Am)) / (40 + long_row + 40 * top(A))).max().item())
+        got = run(build(indptr, cols, m), q, k, v, dy, heads, kv, scale=scale)
+        checked = 0
+        for name in ("y", "dq", "dk", "dv"):
+            value, bound = ref[name]
+            if value.abs().max() < torch.finfo(dtype).max * 0.9:  # (fp16's gradients of the small operand are large)
+                check(got[name], {name: (value, bound * more)}, name)
+                checked += 1
+        assert checked >= 3
+
+
+@pytest.mark.parametrize("longest", [10, 100, 700])
+@pytest.mark.parametrize("keys", [0.0, 30.0])
+def test_values_with_a_common_part(keys, longest):
+    """Values (and keys) that are nearly the same in all columns: t = <dy, v> is nearly D in every entry, and dq = scale sum P (t - D) k is a small difference of
+    large numbers, whichever way it is formed.  In 32 bits the sum over the entries rounds t and D, numbers of the size of T = |dy| |v|; the kernel's
+    sum e t k - D sum e k rounds, per entry, products and sums of the size of T |k| some three times as often: no more than 3 times the error."""
+    heads, c = 2, 16
+    n = max(60, 30_000 // longest)
+    m = max(n, 400)
+    gen = torch.Generator().manual_seed(longest)
+    indptr = torch.arange(n + 1) * longest
+    cols = torch.randint(m, (n * longest,), generator=gen, dtype=torch.int32)
+    r = lambda *s: torch.randn(*s, generator=gen).cuda()
+    q, k, dy, v = r(n, heads * c) / (1 + keys), r(m, heads * c) + keys, r(n, heads * c), r(m, heads * c) + 300 * r(1, heads * c)
+    got = run(build(indptr, cols, m), q, k, v, dy, heads, heads)["dq"].double()
+
+    def by_entries(t):
+        Q, Kk, V, G = (x.to(t).view(-1, heads, c) for x in (q, k, v, dy))
+        j = cols.long().cuda().view(n, longest)
+        s = (Q[:, None] * Kk[j]).sum(3) * c ** -0.5
+        p = torch.softmax(s, 1)
+        x = (G[:, None] * V[j]).sum(3)
+        ds = p * (x - (p * x).sum(1, keepdim=True)) * c ** -0.5
+        return (ds[..., None] * Kk[j]).sum(1).reshape(n, heads * c)
+
+    want, other = by_entries(torch.float64), by_entries(torch.float32).double()
+    assert (got - want).norm() <= 3 * (other - want).norm()
