@@ -1,14 +1,9 @@
 // The attention's entry points (include/isp.h): argument checks, workspaces, dispatch by element type.  The kernels: attention.h.
 #include "attention_args.h"
+#include "elem.h"
 #include "group_stream.h"
 
 namespace {
-
-#define ISP_TRY(call)                   \
-  do {                                  \
-    const isp_status st_ = (call);      \
-    if (st_ != ISP_OK) return st_;      \
-  } while (0)
 
 isp_status check_heads(const isp_csr* A, int32_t heads, int32_t kv_heads, int32_t dh) {
   using namespace isp_dev;
@@ -23,7 +18,7 @@ isp_status check_heads(const isp_csr* A, int32_t heads, int32_t kv_heads, int32_
 }
 isp_status check_operand(const void* p, int64_t ld, int32_t width, int64_t rows, int dtype, const char* name) {
   ISP_TRY(isp_check_dense(p, ld, width, rows, name));
-  if (rows > 0 && ld > 0xffffffffll / (dtype == ISP_F32 ? 4 : 2))
+  if (rows > 0 && ld > 0xffffffffll / isp_dtype_size(dtype))
     return isp_fail(ISP_EUNSUPPORTED, "the rows of %s are 4 GB or more apart", name);
   return ISP_OK;
 }
@@ -33,18 +28,11 @@ isp_status check_type(int dtype, unsigned flags, const isp_csr* A) {
   if ((flags & ISP_BIAS_BY_A) && !A->v.values) return isp_fail(ISP_EINVAL, "ISP_BIAS_BY_A needs a matrix with values");
   return ISP_OK;
 }
-isp_status check_workspace(const void* ws, size_t have, size_t need) {
-  if (need == 0) return ISP_OK;
-  if (!ws) return isp_fail(ISP_EINVAL, "workspace is NULL");
-  if ((uintptr_t)ws & 255) return isp_fail(ISP_EINVAL, "workspace is not 256-byte aligned");
-  if (have < need) return isp_fail(ISP_EINVAL, "workspace too small: %zu < %zu bytes", have, need);
-  return ISP_OK;
-}
 
 size_t forward_bytes(const isp_csr* A, int32_t heads, int32_t dh) { return isp_align((size_t)A->v.n_seg * heads * (dh + 2) * sizeof(float)); }
 // and for the copy of K and V, where the rule takes one
 size_t packed_bytes(const isp_csr* A, int32_t kv_heads, int32_t dh, int dtype, bool whole) {
-  const int64_t row = (int64_t)kv_heads * dh * (dtype == ISP_F32 ? 4 : 2);
+  const int64_t row = (int64_t)kv_heads * dh * isp_dtype_size(dtype);
   return isp_dev::att_packs(row, whole, A->v.nnz, A->v.n_cols) ? (size_t)A->v.n_cols * isp_dev::att_packed_pitch(row) : 0;
 }
 
@@ -83,7 +71,7 @@ isp_status isp_attention_workspace(const isp_csr_t* A, int32_t heads, int32_t kv
   if (!bytes) return isp_fail(ISP_EINVAL, "bytes is NULL");
   ISP_TRY(check_heads(A, heads, kv_heads, head_dim));
   ISP_TRY(check_type(dtype, 0, A));
-  const int64_t row = (int64_t)kv_heads * head_dim * (dtype == ISP_F32 ? 4 : 2);  // (dense rows)
+  const int64_t row = (int64_t)kv_heads * head_dim * isp_dtype_size(dtype);  // (dense rows)
   *bytes = forward_bytes(A, heads, head_dim) + packed_bytes(A, kv_heads, head_dim, dtype, row % isp_dev::ATT_LINE == 0);
   return ISP_OK;
 }
@@ -99,11 +87,11 @@ isp_status isp_attention(const isp_csr_t* A, const void* Q, int64_t ldq, const v
   ISP_TRY(check_operand(K, ldk, kv_heads * head_dim, live * A->v.n_cols, dtype, "K"));
   ISP_TRY(check_operand(V, ldv, kv_heads * head_dim, live * A->v.n_cols, dtype, "V"));
   ISP_TRY(isp_check_dense(Y, ldy, heads * head_dim, A->v.n_rows, "Y"));
-  const uint32_t size = dtype == ISP_F32 ? 4 : 2;
+  const uint32_t size = isp_dtype_size(dtype);
   const auto lines = [&](const void* p, int64_t ld) { return (uintptr_t)p % isp_dev::ATT_LINE == 0 && ld * size % isp_dev::ATT_LINE == 0; };
   const size_t parts = forward_bytes(A, heads, head_dim), copy = packed_bytes(A, kv_heads, head_dim, dtype, lines(K, ldk) && ldv == ldk && (uintptr_t)V % 4 == 0);
   const bool pack = copy && workspace_bytes >= parts + copy;
-  ISP_TRY(check_workspace(workspace, workspace_bytes, parts + (pack ? copy : 0)));
+  ISP_TRY(isp_check_workspace(workspace, workspace_bytes, parts + (pack ? copy : 0)));
   att_args a = make_args(heads, kv_heads, head_dim, scale, flags);
   a.q = Q, a.k = K, a.v = V;
   a.pq = (uint32_t)ldq * size, a.pk = (uint32_t)ldk * size, a.pv = (uint32_t)ldv * size;
@@ -147,8 +135,8 @@ isp_status isp_attention_backward(const isp_csr_t* A, const void* Q, int64_t ldq
   if (dK) ISP_TRY(isp_check_dense(dK, lddk, kv_width, m, "dK"));
   if (dV) ISP_TRY(isp_check_dense(dV, lddv, kv_width, m, "dV"));
   const backward_space b = backward_bytes(A, heads, kv_heads, head_dim);
-  ISP_TRY(check_workspace(workspace, workspace_bytes, b.total));
-  const uint32_t size = dtype == ISP_F32 ? 4 : 2;
+  ISP_TRY(isp_check_workspace(workspace, workspace_bytes, b.total));
+  const uint32_t size = isp_dtype_size(dtype);
   char* ws = static_cast<char*>(workspace);
   att_args a = make_args(heads, kv_heads, head_dim, scale, flags);
   a.q = Q, a.k = K, a.v = V, a.dy = dY;

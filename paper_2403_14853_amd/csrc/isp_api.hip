@@ -73,6 +73,14 @@ isp_status isp_check_dense(const void* p, int64_t ld, int32_t d, int64_t rows, c
   return ISP_OK;
 }
 
+isp_status isp_check_workspace(const void* ws, size_t have, size_t need) {
+  if (need == 0) return ISP_OK;
+  if (!ws) return isp_fail(ISP_EINVAL, "workspace is NULL");
+  if ((uintptr_t)ws & 255) return isp_fail(ISP_EINVAL, "workspace is not 256-byte aligned");
+  if (have < need) return isp_fail(ISP_EINVAL, "workspace too small: %zu < %zu bytes", have, need);
+  return ISP_OK;
+}
+
 extern "C" {
 
 isp_status isp_csr_transpose_workspace(const isp_csr_t* A, size_t* bytes) {

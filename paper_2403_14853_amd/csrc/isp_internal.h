@@ -124,6 +124,11 @@ isp_status isp_fail(isp_status st, const char* fmt, ...);
       return isp_fail(ISP_EHIP, "%s failed: %s (%s:%d)", #call, hipGetErrorString(e_), __FILE__, __LINE__); \
   } while (0)
 #define ISP_LAUNCH_CHECK() ISP_HIP(hipGetLastError())
+#define ISP_TRY(call)                   \
+  do {                                  \
+    const isp_status st_ = (call);      \
+    if (st_ != ISP_OK) return st_;      \
+  } while (0)
 
 static inline size_t isp_align(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -131,6 +136,8 @@ static inline size_t isp_align(size_t x) { return (x + 255) & ~(size_t)255; }
 // The handle's device must be the current one, and an alias must be as recent as its source's values.
 isp_status isp_check_device(const isp_csr* A);
 isp_status isp_check_dense(const void* p, int64_t ld, int32_t d, int64_t rows, const char* name);
+// A call's own workspace of `need` bytes (0: it is not looked at).
+isp_status isp_check_workspace(const void* ws, size_t have, size_t need);
 
 // ---- device scans (scan.hip) -----------------------------------------------------------------
 // Exclusive prefix sums; out has n + 1 entries (out[n] = total).  tmp must hold

@@ -24,7 +24,6 @@ constexpr int LP_GROUP = 1024;              // longest row that a lane group hol
 constexpr int LP_WAVES = 8;                 // wavefronts per workgroup of the streaming kernel
 constexpr int LP_TILE = 1024;               // scores that a wavefront takes at a time
 constexpr int LP_CHUNK = LP_WAVES * LP_TILE;
-constexpr int LP_MAX_TOP = ISP_WAVE;
 
 struct lp_args {
   const void* z;
@@ -479,7 +478,6 @@ __global__ void __launch_bounds__(ISP_WG) k_lp_chunk_bwd(lp_bwd_args g) {
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t LP_THREADS = 1ll << 31;  // of a launch, which has to stay below 2^32 of them
 
 // A wavefront per row where there are rows for all of the chip's wavefronts, or a workgroup would have less than a tile for each of its own.
@@ -487,32 +485,26 @@ bool lp_wave_rows(int64_t n, int classes) { return n >= 4096 || classes <= 2 * L
 // Workgroups per row: one, or, with too few rows for two per compute unit, as many as that takes and the row has chunks for.
 int lp_splits(int64_t n, int classes) {
   if (n == 0 || classes <= LP_GROUP || lp_wave_rows(n, classes)) return 1;
-  const int64_t want = ceil_div(512, n), have = ceil_div(classes, LP_CHUNK);
+  const int64_t want = isp_ceil_div(512, n), have = isp_ceil_div(classes, LP_CHUNK);
   return (int)(want < have ? want : have);
 }
-int lp_lanes(int classes, int vec) {
-  int l = 4;
-  while (l < ISP_WAVE && l * vec < classes) l *= 2;
-  return l;
-}
-
 template <class T, int VEC, int LPR, int NV>
 void lp_group(const lp_args& a, hipStream_t s) {
-  const int64_t g = ceil_div(a.n, ISP_WG / LPR);
+  const int64_t g = isp_ceil_div(a.n, ISP_WG / LPR);
   const unsigned grid = (unsigned)(g < 8192 ? g : 8192);
   if (a.top > 0) k_lp_group<T, VEC, LPR, NV, true><<<grid, ISP_WG, 0, s>>>(a);
   else k_lp_group<T, VEC, LPR, NV, false><<<grid, ISP_WG, 0, s>>>(a);
 }
 template <class T, int VEC, int LPR, int NV>
 void lp_group(const lp_bwd_args& a, hipStream_t s) {
-  const int64_t g = ceil_div(a.n, ISP_WG / LPR);
+  const int64_t g = isp_ceil_div(a.n, ISP_WG / LPR);
   k_lp_group_bwd<T, VEC, LPR, NV><<<(unsigned)(g < 8192 ? g : 8192), ISP_WG, 0, s>>>(a);
 }
 template <class T, class A>
 void lp_short_rows(const A& a, hipStream_t s) {
   constexpr int VEC = 16 / sizeof(T), MAX = 16 / VEC;
   if (a.classes < VEC) return lp_group<T, 1, 8, 1>(a, s);
-  switch (lp_lanes(a.classes, VEC)) {
+  switch (isp_row_lanes(a.classes, VEC)) {
     case 4: return lp_group<T, VEC, 4, 1>(a, s);
     case 8: return lp_group<T, VEC, 8, 1>(a, s);
     case 16: return lp_group<T, VEC, 16, 1>(a, s);
@@ -539,7 +531,7 @@ void lp_run(const lp_args& a, hipStream_t s) {
       if (a.stats) b.stats += 2 * r0;
       if (a.top_logprob) b.top_logprob += r0 * a.top;
       if (a.top_index) b.top_index += r0 * a.top;
-      const unsigned grid = (unsigned)ceil_div(b.n, LP_WAVES);
+      const unsigned grid = (unsigned)isp_ceil_div(b.n, LP_WAVES);
       if (a.top > 0) k_lp_stream<T, 1, true><<<grid, bt, 0, s>>>(b);
       else k_lp_stream<T, 1, false><<<grid, bt, 0, s>>>(b);
     }
@@ -583,7 +575,7 @@ isp_status isp_label_logprob_bwd_launch(const void* Z, int64_t ldz, int64_t n, i
                                         const float* stats, const float* entropy, const float* d_logprob, const float* d_entropy, void* dZ,
                                         int64_t lddz, hipStream_t s) {
   if (n == 0) return ISP_OK;
-  const lp_bwd_args a{Z, ldz, n, n_classes, labels, stats, entropy, d_logprob, d_entropy, dZ, lddz, (int)ceil_div(n_classes, ISP_WG * 16)};
+  const lp_bwd_args a{Z, ldz, n, n_classes, labels, stats, entropy, d_logprob, d_entropy, dZ, lddz, (int)isp_ceil_div(n_classes, ISP_WG * 16)};
   if (dtype == ISP_F32) lp_run<float>(a, s);
   else if (dtype == ISP_BF16) lp_run<bf16_t>(a, s);
   else lp_run<f16_t>(a, s);

@@ -360,20 +360,12 @@ __global__ void __launch_bounds__(LN_COLS* LN_RUNS) k_ln_sums(const float* __res
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
-// Lanes that hold a row: the fewest whose vectors span it, four at least.
-int ln_lanes(int d, int vec) {
-  int l = 4;
-  while (l < ISP_WAVE && l * vec < d) l *= 2;
-  return l;
-}
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 // Workgroups of the backward pass (its rows of sums): as many as there are rows for, up to four per compute unit in lane groups, two or one where a
 // workgroup holds a row, whose sums take as much memory as eight rows of an fp32 matrix per workgroup.
 int64_t ln_bwd_groups(int64_t n, int d) {
   if (d <= LN_GROUP) {
-    const int64_t rows = ISP_WG / ln_lanes(d, 8);  // (of the type with the widest vectors; a bound for both)
-    const int64_t g = ceil_div(n, rows);
+    const int64_t rows = ISP_WG / isp_row_lanes(d, 8);  // (of the type with the widest vectors; a bound for both)
+    const int64_t g = isp_ceil_div(n, rows);
     return g < 1024 ? g : 1024;
   }
   const int64_t most = d <= 4096 ? 512 : d <= LN_BLOCK ? 256 : 64;
@@ -384,7 +376,7 @@ template <class T, int VEC, int LPR, int NV>
 void ln_group(const ln_args& a, bool bwd, hipStream_t s) {
   const int64_t rows = ISP_WG / LPR;
   if (!bwd) {
-    const int64_t g = ceil_div(a.n, rows);
+    const int64_t g = isp_ceil_div(a.n, rows);
     k_ln_fwd<T, VEC, LPR, NV><<<(unsigned)(g < 4096 ? g : 4096), ISP_WG, 0, s>>>(a);
   } else {
     k_ln_bwd<T, VEC, LPR, NV><<<(unsigned)ln_bwd_groups(a.n, a.d), ISP_WG, 0, s>>>(a);
@@ -400,7 +392,7 @@ void ln_run(const ln_args& a, bool bwd, hipStream_t s) {
   constexpr int VEC = 16 / sizeof(T), MAX = LN_REG / VEC;
   if (a.d < VEC) return ln_group<T, 1, 8, 1>(a, bwd, s);
   if (a.d <= LN_GROUP) {
-    switch (ln_lanes(a.d, VEC)) {
+    switch (isp_row_lanes(a.d, VEC)) {
       case 4: return ln_group<T, VEC, 4, 1>(a, bwd, s);
       case 8: return ln_group<T, VEC, 8, 1>(a, bwd, s);
       case 16: return ln_group<T, VEC, 16, 1>(a, bwd, s);
@@ -420,7 +412,7 @@ void ln_run(const ln_args& a, bool bwd, hipStream_t s) {
     return;
   }
   if (a.y) k_ln_bwd_any<T, 1024><<<g, 1024, 0, s>>>(a);
-  if (a.sums) k_ln_sums_any<T, 256><<<dim3((unsigned)ceil_div(a.d, 256), (unsigned)ln_bwd_groups(a.n, a.d)), 256, 0, s>>>(a);
+  if (a.sums) k_ln_sums_any<T, 256><<<dim3((unsigned)isp_ceil_div(a.d, 256), (unsigned)ln_bwd_groups(a.n, a.d)), 256, 0, s>>>(a);
 }
 void ln_dispatch(const ln_args& a, int dtype, bool bwd, hipStream_t s) {
   if (dtype == ISP_F32) ln_run<float>(a, bwd, s);
@@ -456,7 +448,7 @@ isp_status isp_layer_norm_bwd_launch(const void* X, int64_t ldx, const void* dY,
     constexpr int64_t MOST = (1ll << 31) / LN_RUNS;  // columns of a launch, which has to stay below 2^32 threads
     for (int64_t c0 = 0, cols = 2 * (int64_t)d; c0 < cols; c0 += MOST) {
       const int64_t some = cols - c0 < MOST ? cols - c0 : MOST;
-      k_ln_sums<<<(unsigned)ceil_div(some, LN_COLS), LN_COLS * LN_RUNS, 0, s>>>(static_cast<const float*>(ws), rows, d, dweight, dbias, param, c0);
+      k_ln_sums<<<(unsigned)isp_ceil_div(some, LN_COLS), LN_COLS * LN_RUNS, 0, s>>>(static_cast<const float*>(ws), rows, d, dweight, dbias, param, c0);
     }
     ISP_LAUNCH_CHECK();
   }

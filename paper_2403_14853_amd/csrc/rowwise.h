@@ -2,6 +2,16 @@
 #pragma once
 #include "isp_internal.h"
 
+constexpr int ISP_MAX_TOP = ISP_WAVE;  // alternatives: a lane each
+
+static inline int64_t isp_ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Lanes that hold a row of d elements, `vec` to a load: the fewest whose vectors span it, four at least, a wavefront at most.
+static inline int isp_row_lanes(int64_t d, int vec) {
+  int l = 4;
+  while (l < ISP_WAVE && (int64_t)l * vec < d) l *= 2;
+  return l;
+}
+
 size_t isp_layer_norm_sums_bytes(int64_t n, int32_t d);
 isp_status isp_layer_norm_launch(const void* X, int64_t ldx, int64_t n, int32_t d, int dtype, const void* weight, const void* bias, int param,
                                  float eps, void* Y, int64_t ldy, float* mean, float* rstd, hipStream_t s);

@@ -15,18 +15,6 @@ isp_status check_rows(int64_t n, int32_t d) {
   if (d > 2147483647 - 65536) return isp_fail(ISP_EUNSUPPORTED, "rows of %d elements", d);  // (column numbers stay below 2^31)
   return ISP_OK;
 }
-isp_status check_workspace(const void* ws, size_t have, size_t need) {
-  if (need == 0) return ISP_OK;
-  if (!ws) return isp_fail(ISP_EINVAL, "workspace is NULL");
-  if ((uintptr_t)ws & 255) return isp_fail(ISP_EINVAL, "workspace is not 256-byte aligned");
-  if (have < need) return isp_fail(ISP_EINVAL, "workspace too small: %zu < %zu bytes", have, need);
-  return ISP_OK;
-}
-#define ISP_TRY(call)                   \
-  do {                                  \
-    const isp_status st_ = (call);      \
-    if (st_ != ISP_OK) return st_;      \
-  } while (0)
 
 }  // namespace
 
@@ -58,14 +46,14 @@ isp_status isp_layer_norm_backward(const void* X, int64_t ldx, const void* dY, i
   ISP_TRY(isp_check_dense(dY, lddy, d, n, "dY"));
   if (dX) ISP_TRY(isp_check_dense(dX, lddx, d, n, "dX"));
   if (n > 0 && (!mean || !rstd)) return isp_fail(ISP_EINVAL, "mean or rstd is NULL");
-  if (dweight || dbias) ISP_TRY(check_workspace(workspace, workspace_bytes, isp_layer_norm_sums_bytes(n, d)));
+  if (dweight || dbias) ISP_TRY(isp_check_workspace(workspace, workspace_bytes, isp_layer_norm_sums_bytes(n, d)));
   return isp_layer_norm_bwd_launch(X, ldx, dY, lddy, n, d, dtype, weight, param_dtype, mean, rstd, dX, lddx, dweight, dbias, workspace,
                                    (hipStream_t)stream);
 }
 
 static isp_status check_top(int32_t n_classes, int32_t top) {
   if (top < 0 || top > n_classes) return isp_fail(ISP_EINVAL, "top is not in [0, n_classes]");
-  if (top > ISP_WAVE) return isp_fail(ISP_EUNSUPPORTED, "at most %d alternatives", ISP_WAVE);
+  if (top > ISP_MAX_TOP) return isp_fail(ISP_EUNSUPPORTED, "at most %d alternatives", ISP_MAX_TOP);
   return ISP_OK;
 }
 
@@ -85,7 +73,7 @@ isp_status isp_label_logprob(const void* Z, int64_t ldz, int64_t n, int32_t n_cl
   ISP_TRY(check_top(n_classes, top));
   ISP_TRY(isp_check_dense(Z, ldz, n_classes, n, "Z"));
   if (n > 0 && logprob && !labels) return isp_fail(ISP_EINVAL, "labels is NULL");
-  ISP_TRY(check_workspace(workspace, workspace_bytes, isp_label_logprob_parts_bytes(n, n_classes, top)));
+  ISP_TRY(isp_check_workspace(workspace, workspace_bytes, isp_label_logprob_parts_bytes(n, n_classes, top)));
   return isp_label_logprob_launch(Z, ldz, n, n_classes, dtype, labels, logprob, entropy, stats, top, top_logprob, top_index, workspace,
                                   (hipStream_t)stream);
 }
