@@ -11,8 +11,9 @@
 // the group are other workgroups' (blockIdx.y), query heads beyond RQ too (blockIdx.z).  No score is ever written: the backward computes them again.
 //
 // Softmax in one pass: a row's (m, l, y) are a reference for its scores, the sum of exp(s - m) and of exp(s - m) v.  m is the
-// first score, and moves only to a score that is above it by more than ATT_SLACK: the sums stay far from overflow and almost no step has to
-// rescale.  Parts of a row that a run boundary cuts, or a split row's segments, are joined by their references, in a fixed order.
+// first score, and moves only to a score that is above it by more than ATT_SLACK: almost no step has to rescale, and the sums' weights
+// are at most e^8 (values of up to fp32's range over 3000 times the row's entries fit).  The backward's are divided by l: at most 1.  Parts
+// of a row that a run boundary cuts, or a split row's segments, are joined by their references, in a fixed order.
 // In the backward the rows' pass forms D beside dq's two sums, so that y, which has been rounded, is not needed, and leaves it to the
 // columns' pass.
 // Entries whose bias is -inf count for nothing, whatever their operands hold; a row without others has y = 0, l = 0.

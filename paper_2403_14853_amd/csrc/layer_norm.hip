@@ -5,7 +5,8 @@
 //
 // Memory-bound: a row is read once, kept in registers while its mean and then its centred squares are summed (no difference of large
 // sums), and written once.  Up to 1024 columns lane groups hold whole rows (row_lanes.h), so that narrow rows leave no
-// lane idle and need no barrier; up to 16384 a workgroup holds a row; beyond, it passes over the row again.
+// lane idle and need no barrier; up to 16384 a workgroup holds a row (the backward beyond 8192 columns spills 4 registers in fp32 and 38 in fp16:
+// 4,096 x 16,384 170 us = 4.7 TB/s and 109 us = 3.7); beyond, it passes over the row again.
 // The sums over the rows have one accumulator per lane and column while a workgroup passes over its rows; the workgroups' sums are
 // rows of the workspace that a second launch adds, in a fixed order and in 64 bits.  No atomics: results repeat bit for bit.
 #include "row_lanes.h"
