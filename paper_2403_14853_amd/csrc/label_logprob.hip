@@ -4,10 +4,10 @@
 //   dz_j = a (1[j = label] - p_j) - e p_j (log p_j + S),  a, e the upstream gradients of log p_label and S
 // One pass over the scores, in 32 bits: rows of up to 1024 scores lie in the registers of a lane group (row_lanes.h); longer ones are streamed
 // with a running maximum per lane, to which T and U are rescaled once per 16 scores, by a wavefront, by the eight of a
-// workgroup, or, where there are few rows, by several workgroups whose parts a second launch joins.  The exponential and five more
-// instructions per score keep pace with the loads of long rows (2,053 x 65,521, bf16: 80 us = 3.4 TB/s, vector ALU 41 % busy).  On rows of tens of scores
-// the sums over lanes and the row's end come to as much again, and the vector ALU bounds the forward (2.45 M x 47, bf16: 102 us, 63 % busy at 2.9 TB/s of
-// misses); the backward is bound by memory (129 us, 4.2 TB/s).
+// workgroup, or, where there are few rows, by several workgroups whose parts a second launch joins.  Ten vector
+// instructions per score, an exponential among them, keep pace with the loads of long rows (2,053 x 65,521, bf16: 80 us = 3.4 TB/s, vector ALU 41 % busy).
+// On rows of tens of scores the sums over lanes and the row's end come to as much again (21 per score), and the vector ALU bounds the forward (2.45 M x 47,
+// bf16: 102 us, 63 % busy at 2.9 TB/s of misses); the backward is bound by memory (129 us, 4.2 TB/s).
 // What a row holds decides: -inf is a class left out (p = 0); a row with nothing left has log probabilities of -inf, entropy 0 and no gradient;
 // NaN and +inf make the row's results NaN.
 //

@@ -615,3 +615,22 @@ def test_values_with_a_common_part(keys, longest):
 
     want, other = by_entries(torch.float64), by_entries(torch.float32).double()
     assert (got - want).norm() <= 3 * (other - want).norm()
+
+
+def test_on_another_stream():
+    """Both passes on a stream of the caller's, with workspaces of their own; outputs and statistics are there, filled, before the calls."""
+    n, m, heads, kv, c = 3000, 2500, 8, 4, 16
+    indptr, cols = graph(n, m, 12, hubs=((100, 6000), (900, 2000)))
+    A = build(indptr, cols, m)
+    q, k, v, dy = operands(n, m, heads, kv, c, torch.bfloat16, seed=1)
+    want = run(A, q, k, v, dy, heads, kv)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        outs = [torch.full_like(t, 99.0) for t in (q, q, k, v)]
+        stats = torch.full((n, heads, 2), 99.0, device="cuda")
+        torch.cuda.synchronize()
+        isp.attention(A, q, k, v, outs[0], heads, kv, stats=stats, stream=side)
+        isp.attention_backward(A, q, k, v, stats, dy, *outs[1:], heads, kv, stream=side)
+        side.synchronize()
+        for t, name in zip(outs, ("y", "dq", "dk", "dv")):
+            assert torch.equal(t, want[name]), name
